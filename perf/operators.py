@@ -136,8 +136,9 @@ def _quantize(x, fmt, m):
     a = x.abs().amax(-1)
     if fmt == "nvfp4":
         m = _largest(m)
-        s = (a * (448.0 / m)).clamp(max=448.0).to(torch.float8_e4m3fn)
-        r = torch.where(s.float() > 0, (2688.0 / m) / s.float(), 0.0)
+        # a number over a tensor is its reciprocal times the number, which rounds twice
+        s = (a * (torch.full_like(m, 448.0) / m)).clamp(max=448.0).to(torch.float8_e4m3fn)
+        r = torch.where(s.float() > 0, (torch.full_like(m, 2688.0) / m) / s.float(), 0.0)
         return _e2m1(x * r[..., None]), s.view(torch.uint8), s.float()
     e = (_floor_log2(a) - (2 if fmt == "mxfp4" else 0)).clamp(min=-127)
     v = x * _pow2(-e)[..., None]
