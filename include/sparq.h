@@ -303,6 +303,96 @@ SPARQ_API int sparq_quantize_act_u8(const void *x, int dtype, size_t n, const fl
 SPARQ_API int sparq_quantize_weight_s8(const float *w, int64_t cout, int64_t k, int8_t *out, float *scale_out,
                              void *stream);
 
+/* ---- Microscaled formats -------------------------------------------------------------------
+ * Block-scaled formats of a few bits per element, for layers whose activations SPARQ's 8-bit
+ * grid does not suit (signed, with outliers: language models) and for training.  Not in the
+ * paper.  A block is a run of consecutive elements of a row; `a` is its largest magnitude.
+ *   SPARQ_MXFP4   32 e2m1 elements (0 .5 1 1.5 2 3 4 6 and their negatives), scale
+ *                 2^(floor(log2 a) - 2).  value = q * scale
+ *   SPARQ_NVFP4   16 e2m1 elements, scale s = e4m3(a * (448 / m)), and m, the largest magnitude of
+ *                 the whole tensor, in fp32 (what sparq_absmax gathers).  q = e2m1(x * ((2688 / m) / s)),
+ *                 0 where s is 0.  value = q * s * (m / 2688)
+ *   SPARQ_MXINT8  32 signed 8-bit elements in units of 2^-6, scale 2^floor(log2 a).
+ *                 q = clamp(rint(x * 2^6 / scale), -127, 127).  value = q * 2^-6 * scale
+ * fp32 arithmetic, one IEEE operation per step as written; e2m1 and e4m3 round to nearest even and
+ * saturate (6; 448).  Powers of two are at least 2^-127, which blocks of zeros and of subnormals take.
+ * m below 2^-100 counts as 2^-100; larger values than m saturate.  A block that holds an infinity
+ * or a NaN has codes of zero and the scale's NaN (0xFF; 0x7F in e4m3): it reads as NaN throughout.
+ * Memory: a row's codes take round_up(cols, 32) elements, those past cols are zeros; of 4-bit
+ * elements the even one is in the low half of its byte.  A 4-bit format's scales form tiles of
+ * 128 rows x 4 scales, 512 bytes each: row r, scale c at byte (r % 32) * 16 + (r % 128) / 32 * 4 + c % 4 of
+ * tile (r / 128) * ceil(C / 4) + c / 4, C scales a row; padding is zero.  MXINT8's scales lie row by row,
+ * each row padded with zeros to a multiple of 16 bytes.  e8m0 scales are stored as exponent + 127.
+ * Codes and scales are caller-owned and 16-byte aligned (else SPARQ_ERR_UNSUPPORTED). */
+enum { SPARQ_MXFP4 = 0, SPARQ_NVFP4 = 1, SPARQ_MXINT8 = 2 };
+
+/* Bytes of a rows x cols tensor's codes and of its scales, or a negative sparq_status. */
+SPARQ_API int64_t sparq_mx_code_bytes(int format, int64_t rows, int64_t cols);
+SPARQ_API int64_t sparq_mx_scale_bytes(int format, int64_t rows, int64_t cols);
+
+/* x: rows x cols of fp32 or bf16 (SPARQ_DTYPE_*), row r at x + r * ldx elements, ldx >= cols; any
+ * alignment of its elements (rows that start on 32-byte boundaries are fastest).  max_dev: m on the
+ * DEVICE, for SPARQ_NVFP4 only (NULL else).  Writes codes and scales, padding included.  rows == 0 or cols == 0
+ * is a no-op. */
+SPARQ_API int sparq_quantize_mx(const void *x, int dtype, int64_t rows, int64_t cols, int64_t ldx, int format,
+                      const float *max_dev, void *codes, uint8_t *scales, void *stream);
+
+/* out[r][c] = value, rounded to nearest even for bf16 (exact for MXFP4 and MXINT8).  ldo >= cols; what
+ * lies between the rows is left as it is. */
+SPARQ_API int sparq_dequantize_mx(const void *codes, const uint8_t *scales, int64_t rows, int64_t cols, int format,
+                        const float *max_dev, void *out, int dtype, int64_t ldo, void *stream);
+
+/* What happens to a 4-bit product.  For output column j, in fp32 and in this order:
+ *     t = acc * ((a_max / 2688) * (b_max / 2688))     (SPARQ_NVFP4 only)
+ *     y = t + bias[j];  if (relu) y = y > 0 ? y : 0;  f32_out = y;  bf16_out = y to nearest even
+ * Outputs are M x N row-major with leading dimension N; at least one must be non-NULL. */
+typedef struct {
+    const float *a_max, *b_max;   /* DEVICE: m of A and of B, for SPARQ_NVFP4; NULL else */
+    const float *bias;            /* [N] device, or NULL */
+    int32_t relu;                 /* 0 / 1 */
+    float *f32_out;               /* or NULL */
+    void *bf16_out;               /* or NULL */
+} sparq_mx_epilogue;
+
+/* acc[m][j] = sum_k A[m][k] * B[j][k] of two tensors in the same 4-bit format, without the tensors' own
+ * scales: A is M x K, B is N x K (the layout of a linear layer's weights), codes and scales as
+ * sparq_quantize_mx leaves them.  Products are exact, sums are held in fp32 in an order that depends on the sizes only.
+ * K >= 1; M == 0 or N == 0 is a no-op.  M, N and K below 2^31 - 256 (else SPARQ_ERR_UNSUPPORTED). */
+SPARQ_API int sparq_gemm_mxf4(const void *A, const uint8_t *A_scales, const void *B, const uint8_t *B_scales,
+                    int64_t M, int64_t N, int64_t K, int format, const sparq_mx_epilogue *e, void *stream);
+
+/* Activation functions whose inputs are kept in 8 bits for the backward pass.
+ *     IDENTITY x    RELU x > 0 ? x : 0    SILU x / (1 + exp(-x))
+ *     GELU     x / (1 + exp(-2 sqrt(2/pi) (x + 0.044715 x^3)))        (the form with tanh)
+ * in fp32, the exponential and the quotient approximate to a few units of the last place. */
+enum { SPARQ_ACT_IDENTITY = 0, SPARQ_ACT_RELU = 1, SPARQ_ACT_SILU = 2, SPARQ_ACT_GELU = 3 };
+
+/* y = act(x), or act(x) * up where up is not NULL (the gate and up projections of a gated feed-forward
+ * block: two matrices of the same leading dimension, one matrix's halves included), and x and up as
+ * SPARQ_MXINT8 in the same pass: codes / scales and up_codes / up_scales, of the sizes of
+ * sparq_mx_*_bytes.  up_codes and up_scales are NULL without up.  y has x's dtype and may be x or up
+ * itself (same leading dimension), else it overlaps neither. */
+SPARQ_API int sparq_act_forward_mx8(const void *x, const void *up, int dtype, int64_t rows, int64_t cols, int64_t ldx, int act,
+                          void *y, int64_t ldy, int8_t *codes, uint8_t *scales, int8_t *up_codes, uint8_t *up_scales,
+                          void *stream);
+
+/* The backward pass, from the kept values x^ and up^:
+ *     dx = dy * act'(x^);  with up: dx = (dy * up^) * act'(x^), dup = dy * act(x^).
+ * dx and dup share lddx; dx or dup may be dy itself (same leading dimension).  A block that reads as NaN gives
+ * NaN. */
+SPARQ_API int sparq_act_backward_mx8(const void *dy, int dtype, int64_t rows, int64_t cols, int64_t lddy, int act,
+                           const int8_t *codes, const uint8_t *scales, const int8_t *up_codes, const uint8_t *up_scales,
+                           void *dx, void *dup, int64_t lddx, void *stream);
+
+/* Gradient of a linear layer's weights from its input X kept as SPARQ_MXINT8 (M tokens x K):
+ *     dw[j][k] = sum_m dy[m][j] * X[m][k]   (+ dw[j][k] where accumulate is not 0)
+ * dy is M x N bf16, row m at dy + m * lddy; dw is N x K fp32 with leading dimension K.  Products are
+ * exact, sums are held in fp32 in an order that depends on the sizes only.  M == 0 leaves dw zero (as it is, accumulating).
+ * Requirements (else SPARQ_ERR_UNSUPPORTED): dy 16-byte aligned, lddy a multiple of 8, dw aligned to its
+ * elements, M, N and K below 2^31 - 256. */
+SPARQ_API int sparq_wgrad_mx8(const void *dy, int64_t lddy, const int8_t *codes, const uint8_t *scales,
+                    int64_t M, int64_t N, int64_t K, int accumulate, float *dw, void *stream);
+
 /* ---- 2:4 sparse weights (Sections 4 and 5.3) ---------------------------------------------
  * Weights pruned 2:4 arrive compressed as a sparse tensor core stores them: per output
  * channel j and per group of four consecutive reduction indices, the two kept values

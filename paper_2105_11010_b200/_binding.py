@@ -42,6 +42,11 @@ class _CEpilogue(ctypes.Structure):
                 ("residual", ctypes.c_void_p), ("residual_scale", ctypes.c_float)]
 
 
+class _CMxEpilogue(ctypes.Structure):
+    _fields_ = [("a_max", ctypes.c_void_p), ("b_max", ctypes.c_void_p), ("bias", ctypes.c_void_p),
+                ("relu", ctypes.c_int32), ("f32_out", ctypes.c_void_p), ("bf16_out", ctypes.c_void_p)]
+
+
 @dataclass(frozen=True)
 class SparqParams:
     """Mirror of ``sparq_params``."""
@@ -101,6 +106,17 @@ def load_library() -> ctypes.CDLL:
         L.sparq_gemm_s8_sparse24.argtypes = [vp, vp, i64, i64, i64, ctypes.POINTER(_CParams),
                                              ctypes.POINTER(_CEpilogue), vp, vp]
         L.sparq_gemm_s8_sparse24.restype = i32
+        for f in (L.sparq_mx_code_bytes, L.sparq_mx_scale_bytes):
+            f.argtypes, f.restype = [i32, i64, i64], i64
+        L.sparq_quantize_mx.argtypes = [vp, i32, i64, i64, i64, i32, vp, vp, vp, vp]
+        L.sparq_dequantize_mx.argtypes = [vp, vp, i64, i64, i32, vp, vp, i32, i64, vp]
+        L.sparq_gemm_mxf4.argtypes = [vp, vp, vp, vp, i64, i64, i64, i32, ctypes.POINTER(_CMxEpilogue), vp]
+        L.sparq_act_forward_mx8.argtypes = [vp, vp, i32, i64, i64, i64, i32, vp, i64, vp, vp, vp, vp, vp]
+        L.sparq_act_backward_mx8.argtypes = [vp, i32, i64, i64, i64, i32, vp, vp, vp, vp, vp, vp, i64, vp]
+        L.sparq_wgrad_mx8.argtypes = [vp, i64, vp, vp, i64, i64, i64, i32, vp, vp]
+        for f in (L.sparq_quantize_mx, L.sparq_dequantize_mx, L.sparq_gemm_mxf4, L.sparq_act_forward_mx8,
+                  L.sparq_act_backward_mx8, L.sparq_wgrad_mx8):
+            f.restype = i32
         L.sparq_quantize_host.argtypes = L.sparq_quantize.argtypes
         L.sparq_quantize_host.restype = i32
         L.sparq_gemm_s8_host.argtypes = L.sparq_gemm_s8.argtypes
@@ -347,6 +363,84 @@ def sparq_gemm_s8_sparse24(A: torch.Tensor, w_exp: torch.Tensor, params: SparqPa
     :func:`sparq_sparse24_expand_weights`, then the epilogue."""
     rc = _native.gemm_sparse24(A, w_exp, params, workspace, scale, bias, relu, inv_out_scale, acc_out, f32_out, u8_out,
                                None, None, 0.0, stream)
+    if rc:
+        _raise(rc)
+
+
+# ---- microscaled formats --------------------------------------------------------------------
+
+FORMAT_MXFP4, FORMAT_NVFP4, FORMAT_MXINT8 = 0, 1, 2
+ACT_IDENTITY, ACT_RELU, ACT_SILU, ACT_GELU = 0, 1, 2, 3
+
+
+def sparq_mx_code_bytes(fmt: int, rows: int, cols: int) -> int:
+    """Bytes of a tensor's codes: rows of round_up(cols, 32) elements (uint8 (rows, that / 2) for the
+    4-bit formats, int8 (rows, that) for MXINT8)."""
+    rc = load_library().sparq_mx_code_bytes(int(fmt), int(rows), int(cols))
+    if rc < 0:
+        _raise(int(rc))
+    return int(rc)
+
+
+def sparq_mx_scale_bytes(fmt: int, rows: int, cols: int) -> int:
+    """Bytes of a tensor's scales, padding included (uint8)."""
+    rc = load_library().sparq_mx_scale_bytes(int(fmt), int(rows), int(cols))
+    if rc < 0:
+        _raise(int(rc))
+    return int(rc)
+
+
+def sparq_quantize_mx(x: torch.Tensor, fmt: int, codes: torch.Tensor, scales: torch.Tensor, *,
+                      max_dev: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Codes and scales of the matrix ``x`` (float32 or bfloat16, rows contiguous, any row pitch) in a
+    microscaled format.  ``max_dev`` (float32, 1 element): the tensor's largest magnitude, NVFP4 only."""
+    rc = _native.quantize_mx(x, fmt, codes, scales, max_dev, stream)
+    if rc:
+        _raise(rc)
+
+
+def sparq_dequantize_mx(codes: torch.Tensor, scales: torch.Tensor, fmt: int, out: torch.Tensor, *,
+                        max_dev: Optional[torch.Tensor] = None, stream=None) -> None:
+    """The matrix that codes and scales stand for, in ``out`` (float32 or bfloat16)."""
+    rc = _native.dequantize_mx(out, fmt, codes, scales, max_dev, stream)
+    if rc:
+        _raise(rc)
+
+
+def sparq_gemm_mxf4(A: torch.Tensor, A_scales: torch.Tensor, B: torch.Tensor, B_scales: torch.Tensor, fmt: int, *,
+                    a_max: Optional[torch.Tensor] = None, b_max: Optional[torch.Tensor] = None,
+                    bias: Optional[torch.Tensor] = None, relu: bool = False,
+                    f32_out: Optional[torch.Tensor] = None, bf16_out: Optional[torch.Tensor] = None,
+                    stream=None) -> None:
+    """``A @ B^T`` of two matrices in the same 4-bit format (codes ``(M, K/2)`` and ``(N, K/2)`` uint8), plus
+    ``bias``, then ReLU if asked for."""
+    rc = _native.gemm_mxf4(A, A_scales, B, B_scales, fmt, a_max, b_max, bias, relu, f32_out, bf16_out, stream)
+    if rc:
+        _raise(rc)
+
+
+def sparq_act_forward_mx8(x: torch.Tensor, act: int, y: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, *,
+                          up: Optional[torch.Tensor] = None, up_codes: Optional[torch.Tensor] = None,
+                          up_scales: Optional[torch.Tensor] = None, stream=None) -> None:
+    """``y = act(x)``, or ``act(x) * up``, and ``x`` (and ``up``) kept as MXINT8 for the backward pass."""
+    rc = _native.act_forward_mx8(x, act, y, codes, scales, up, up_codes, up_scales, stream)
+    if rc:
+        _raise(rc)
+
+
+def sparq_act_backward_mx8(dy: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, act: int, dx: torch.Tensor, *,
+                           up_codes: Optional[torch.Tensor] = None, up_scales: Optional[torch.Tensor] = None,
+                           dup: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Gradients of :func:`sparq_act_forward_mx8` from what it kept: ``dx``, and ``dup`` with a gate."""
+    rc = _native.act_backward_mx8(dy, act, codes, scales, dx, up_codes, up_scales, dup, stream)
+    if rc:
+        _raise(rc)
+
+
+def sparq_wgrad_mx8(dy: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, dw: torch.Tensor, *,
+                    accumulate: bool = False, stream=None) -> None:
+    """``dw (N, K) = dy^T @ X`` (``+ dw``) with ``dy`` (M, N) bfloat16 and X (M, K) kept as MXINT8."""
+    rc = _native.wgrad_mx8(dy, codes, scales, dw, accumulate, stream)
     if rc:
         _raise(rc)
 

@@ -28,6 +28,9 @@ struct XformArgs {
 // Checks `p` (Section 3.1 placement sets, Section 5.1 widths) and fills `x`.
 int validate_params(const sparq_params *p, XformArgs *x);
 
+// SPARQ_OK for SPARQ_DTYPE_F32 and SPARQ_DTYPE_BF16 (sparq_frontend.cu).
+int check_dtype(int dtype);
+
 // Device status word shared by all kernels of this library on the current device.
 // Bit 0: a bounded wait expired.  Allocated on first use, freed by sparq_shutdown().
 int get_status_word(unsigned int **dptr);

@@ -240,14 +240,14 @@ int stream_grid(size_t nvec, int *blocks)
     return SPARQ_OK;
 }
 
+}  // namespace
+
 int check_dtype(int dtype)
 {
     if (dtype != SPARQ_DTYPE_F32 && dtype != SPARQ_DTYPE_BF16)
         return set_error(SPARQ_ERR_INVALID_ARG, "dtype %d is neither SPARQ_DTYPE_F32 nor SPARQ_DTYPE_BF16", dtype);
     return SPARQ_OK;
 }
-
-}  // namespace
 
 }  // namespace sparq
 

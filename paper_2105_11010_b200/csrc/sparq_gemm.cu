@@ -78,26 +78,33 @@ static void map_store(const MapKey &k, const CUtensorMap &m)
     s.used = true; s.key = k; s.map = m;
 }
 
-// 2-D K-contiguous matrix [rows][K] with row pitch ld bytes; box = bk x box_rows.
-static int encode_2d(CUtensorMap *map, const void *ptr, int64_t K, int64_t rows, int64_t ld, int bk, int box_rows)
+// Matrix of `rows` rows of `inner` elements, `pitch` bytes apart, read in boxes (sparq_gemm_kernel.cuh).
+int encode_matrix(CUtensorMap *map, CUtensorMapDataType type, const void *ptr, int64_t inner, int64_t rows, int64_t pitch, int box_inner,
+                  int box_rows, CUtensorMapSwizzle swizzle)
 {
     static EncodeTiledFn fn = nullptr;
     if (!fn) {
         int rc = driver_fn("cuTensorMapEncodeTiled", (void **)&fn);
         if (rc != SPARQ_OK) return rc;
     }
-    const MapKey key = {{1, (uint64_t)(uintptr_t)ptr, (uint64_t)K, (uint64_t)rows, (uint64_t)ld, (uint64_t)bk, (uint64_t)box_rows}};
+    const MapKey key = {{1, (uint64_t)(uintptr_t)ptr, (uint64_t)inner, (uint64_t)rows, (uint64_t)pitch, (uint64_t)box_inner, (uint64_t)box_rows,
+                         (uint64_t)type, (uint64_t)swizzle}};
     if (map_lookup(key, map)) return SPARQ_OK;
-    cuuint64_t dims[2] = {(cuuint64_t)K, (cuuint64_t)rows};
-    cuuint64_t strides[1] = {(cuuint64_t)ld};
-    cuuint32_t box[2] = {(cuuint32_t)bk, (cuuint32_t)box_rows};
+    cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)rows};
+    cuuint64_t strides[1] = {(cuuint64_t)pitch};
+    cuuint32_t box[2] = {(cuuint32_t)box_inner, (cuuint32_t)box_rows};
     cuuint32_t estr[2] = {1, 1};
-    CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(ptr), dims, strides, box, estr,
-                    CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle_for(bk), CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    CUresult r = fn(map, type, 2, const_cast<void *>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) return set_error(SPARQ_ERR_CUDA, "cuTensorMapEncodeTiled failed with CUresult %d", (int)r);
     map_store(key, *map);
     return SPARQ_OK;
+}
+
+// 2-D K-contiguous matrix [rows][K] with row pitch ld bytes; box = bk x box_rows.
+static int encode_2d(CUtensorMap *map, const void *ptr, int64_t K, int64_t rows, int64_t ld, int bk, int box_rows)
+{
+    return encode_matrix(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, ptr, K, rows, ld, bk, box_rows, swizzle_for(bk));
 }
 
 // The weight matrix [rows][K] in groups of 32 rows (rows a multiple of 32).  Row 8j + 2q + b of a group in
@@ -158,7 +165,7 @@ static int encode_im2col(CUtensorMap *map, const void *ptr, int n, int h, int w,
     return SPARQ_OK;
 }
 
-static int device_info(int *sms)
+int device_info(int *sms)
 {
     int dev = 0, major = 0;
     cudaError_t e = cudaGetDevice(&dev);

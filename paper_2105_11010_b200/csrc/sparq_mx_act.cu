@@ -1,0 +1,228 @@
+// Activation functions whose inputs are kept for the backward pass in 8 bits (MXINT8), and that backward pass.
+//
+//   forward    y = act(x)             or act(x) * up        from x and up as they are; both also go out as codes
+//   backward   dx = dy * act'(x^)     or dy * up^ * act'(x^) and dup = dy * act(x^), x^ and up^ what the codes stand for
+//
+// silu(x) = x s(x) and gelu(x) = x s(2 sqrt(2/pi) (x + 0.044715 x^3)), the form with tanh, are both x s(z(x)) with
+// s the logistic function: act' = s + x s (1 - s) z'.
+//
+// A thread takes 16 elements of a row as in sparq_mx.cu.  Every tensor is read and written once: HBM traffic is the bound,
+// 7 bytes forward and 8 backward per element of a gated bf16 pair.
+#include "sparq_mx.cuh"
+
+namespace sparq {
+
+namespace {
+
+constexpr float kGeluScale = 1.5957691216057308f;      // 2 sqrt(2 / pi)
+constexpr float kGeluCubic = 0.044715f;
+
+// 1 / (1 + exp(-z)); the approximate exponential and quotient are within a few units of 2^-24 of it.
+__device__ __forceinline__ float logistic(float z) { return __fdividef(1.0f, 1.0f + __expf(-z)); }
+
+template <int ACT>
+__device__ __forceinline__ float act_value(float x)
+{
+    if (ACT == SPARQ_ACT_IDENTITY) return x;
+    if (ACT == SPARQ_ACT_RELU) return x > 0.0f ? x : 0.0f;
+    if (ACT == SPARQ_ACT_SILU) return x * logistic(x);
+    return x * logistic(kGeluScale * x * __fmaf_rn(kGeluCubic * x, x, 1.0f));
+}
+
+// act(x) and act'(x) of a number.
+template <int ACT>
+__device__ __forceinline__ void act_both(float x, float &y, float &d)
+{
+    if (ACT == SPARQ_ACT_IDENTITY) {
+        y = x;
+        d = 1.0f;
+    } else if (ACT == SPARQ_ACT_RELU) {
+        y = x > 0.0f ? x : 0.0f;
+        d = x > 0.0f ? 1.0f : 0.0f;
+    } else {
+        // s is 0 or 1 to the last bit long before |x| = 64, and x^3 overflows far behind it
+        const float c = ACT == SPARQ_ACT_SILU ? fminf(fmaxf(x, -128.0f), 128.0f) : fminf(fmaxf(x, -64.0f), 64.0f);
+        const float z = ACT == SPARQ_ACT_SILU ? c : kGeluScale * c * __fmaf_rn(kGeluCubic * c, c, 1.0f);
+        const float dz = ACT == SPARQ_ACT_SILU ? 1.0f : __fmaf_rn(3.0f * kGeluCubic * kGeluScale * c, c, kGeluScale);
+        const float s = logistic(z);
+        y = x * s;
+        d = __fmaf_rn(c * s * (1.0f - s), dz, s);
+    }
+}
+
+// Codes and scale of a run, its block's other half in the neighbouring lane.
+__device__ __forceinline__ void keep_run(const float (&f)[16], bool coded, int64_t row, int64_t run, int64_t pitch, int64_t words,
+                                         int8_t *codes, uint8_t *scales)
+{
+    uint32_t mb = run_max_bits(f);
+    mb = max(mb, __shfl_xor_sync(0xFFFFFFFFu, mb, 1));
+    uint32_t code = e8m0_code(mb, 0u);
+    if (coded) {
+        const uint4 w = int8_codes(f, inv_pow2_of_code(code));
+        reinterpret_cast<uint4 *>(codes + row * pitch)[run] = mb >= kInfBits ? make_uint4(0u, 0u, 0u, 0u) : w;
+    } else {
+        code = 0u;
+    }
+    const uint32_t word = gather_word<8>(code);
+    if ((threadIdx.x & 7) == 0) *reinterpret_cast<uint32_t *>(scales + mx_scale_word<false>(row, run >> 3, words)) = word;
+}
+
+struct ActForward {
+    const void *x, *up;
+    int64_t rows, cols, ldx, ldy, per_row;
+    void *y;
+    int8_t *codes, *up_codes;
+    uint8_t *scales, *up_scales;
+};
+
+template <bool BF16, int ALIGN, int ACT, bool GATED>
+__global__ void __launch_bounds__(kRunThreads)
+act_forward_mx8_kernel(const ActForward g)
+{
+    constexpr int kWidth = BF16 ? 2 : 4;
+    const int64_t stride = (int64_t)gridDim.x * kRunThreads, first = (int64_t)blockIdx.x * kRunThreads + threadIdx.x;
+    const int64_t pitch = mx_padded(g.cols), words = mx_scale_cols(SPARQ_MXINT8, g.cols) / 4, runs = g.rows * g.per_row;
+    RunWalk at(first, stride, g.per_row);
+    dep_wait();
+    dep_launch();
+    // per_row is a multiple of 32: a warp's lanes share a row and leave the loop together
+    for (int64_t i = first; i < runs; i += stride, at.next()) {
+        const int64_t left = g.cols - at.run * 16, off = left > 0 ? (at.row * g.ldx + at.run * 16) * kWidth : 0;
+        const bool coded = at.run * 16 < pitch;
+        float f[16], u[16];
+        load_run<BF16, ALIGN>(f, reinterpret_cast<const uint8_t *>(g.x) + off, left);
+        if (GATED) load_run<BF16, ALIGN>(u, reinterpret_cast<const uint8_t *>(g.up) + off, left);
+        keep_run(f, coded, at.row, at.run, pitch, words, g.codes, g.scales);
+        if (GATED) keep_run(u, coded, at.row, at.run, pitch, words, g.up_codes, g.up_scales);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            f[j] = act_value<ACT>(f[j]);
+            if (GATED) f[j] = __fmul_rn(f[j], u[j]);
+        }
+        if (left > 0) store_run<BF16, ALIGN>(reinterpret_cast<uint8_t *>(g.y) + (at.row * g.ldy + at.run * 16) * kWidth, f, left);
+    }
+}
+
+struct ActBackward {
+    const void *dy;
+    const int8_t *codes, *up_codes;
+    const uint8_t *scales, *up_scales;
+    int64_t rows, cols, lddy, lddx, per_row;
+    void *dx, *dup;
+};
+
+template <bool BF16, int ALIGN, int ACT, bool GATED>
+__global__ void __launch_bounds__(kRunThreads)
+act_backward_mx8_kernel(const ActBackward g)
+{
+    constexpr int kWidth = BF16 ? 2 : 4;
+    const int64_t stride = (int64_t)gridDim.x * kRunThreads, first = (int64_t)blockIdx.x * kRunThreads + threadIdx.x;
+    const int64_t pitch = mx_padded(g.cols), words = mx_scale_cols(SPARQ_MXINT8, g.cols) / 4, runs = g.rows * g.per_row;
+    RunWalk at(first, stride, g.per_row);
+    dep_wait();
+    dep_launch();
+    for (int64_t i = first; i < runs; i += stride, at.next()) {
+        const int64_t left = g.cols - at.run * 16;
+        const int64_t sc = mx_scale_word<false>(at.row, at.run >> 3, words) + ((at.run >> 1) & 3);
+        float dy[16], x[16], u[16];
+        load_run<BF16, ALIGN>(dy, reinterpret_cast<const uint8_t *>(g.dy) + (at.row * g.lddy + at.run * 16) * kWidth, left);
+        const uint32_t scale = g.scales[sc];
+        floats_of_int8(x, reinterpret_cast<const uint4 *>(g.codes + at.row * pitch)[at.run], scale);
+        if (GATED) floats_of_int8(u, reinterpret_cast<const uint4 *>(g.up_codes + at.row * pitch)[at.run], g.up_scales[sc]);
+        const bool nan = scale == kNanE8M0;           // comparisons and minima would lose it
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            float y, d;
+            act_both<ACT>(x[j], y, d);
+            if (nan) y = d = x[j];
+            const float t = dy[j];
+            dy[j] = __fmul_rn(GATED ? __fmul_rn(t, u[j]) : t, d);
+            if (GATED) u[j] = __fmul_rn(t, y);
+        }
+        const int64_t off = (at.row * g.lddx + at.run * 16) * kWidth;
+        store_run<BF16, ALIGN>(reinterpret_cast<uint8_t *>(g.dx) + off, dy, left);
+        if (GATED) store_run<BF16, ALIGN>(reinterpret_cast<uint8_t *>(g.dup) + off, u, left);
+    }
+}
+
+int check_act(int dtype, int act, int64_t rows, int64_t cols)
+{
+    const int rc = check_dtype(dtype);
+    if (rc != SPARQ_OK) return rc;
+    if (act < SPARQ_ACT_IDENTITY || act > SPARQ_ACT_GELU) return set_error(SPARQ_ERR_INVALID_ARG, "act %d is not one of SPARQ_ACT_*", act);
+    if (rows < 0 || cols < 0) return set_error(SPARQ_ERR_INVALID_ARG, "negative dimension");
+    return SPARQ_OK;
+}
+
+int check_pitches(int dtype, int64_t rows, int64_t cols, int64_t lda, int64_t ldb, uintptr_t values, uintptr_t kept)
+{
+    if (lda < cols || ldb < cols) return set_error(SPARQ_ERR_INVALID_ARG, "a leading dimension is less than the columns (%lld)", (long long)cols);
+    if (values & (dtype == SPARQ_DTYPE_BF16 ? 1u : 3u)) return set_error(SPARQ_ERR_UNSUPPORTED, "a tensor is not aligned to its elements");
+    if (kept & 15u) return set_error(SPARQ_ERR_UNSUPPORTED, "codes and scales must be 16-byte aligned");
+    const int64_t ld = lda > ldb ? lda : ldb;
+    if (rows > INT64_C(1) << 40 || ld > INT64_C(1) << 40 || (__int128)rows * (ld + 512) > INT64_C(1) << 60)
+        return set_error(SPARQ_ERR_UNSUPPORTED, "%lld rows of %lld elements are more than any device holds", (long long)rows, (long long)ld);
+    return SPARQ_OK;
+}
+
+int min_align(int a, int b) { return a < b ? a : b; }
+
+}  // namespace
+
+}  // namespace sparq
+
+using namespace sparq;
+
+#define SPARQ_ACT_PICK_A(KERNEL, B, align, ACT, GATED)                                                                  \
+    ((align) == 32 ? KERNEL<B, 32, ACT, GATED> : (align) == 16 ? KERNEL<B, 16, ACT, GATED> : KERNEL<B, 0, ACT, GATED>)
+#define SPARQ_ACT_PICK_G(KERNEL, bf16, align, ACT, gated)                                                               \
+    ((bf16) ? ((gated) ? SPARQ_ACT_PICK_A(KERNEL, true, align, ACT, true) : SPARQ_ACT_PICK_A(KERNEL, true, align, ACT, false))   \
+            : ((gated) ? SPARQ_ACT_PICK_A(KERNEL, false, align, ACT, true) : SPARQ_ACT_PICK_A(KERNEL, false, align, ACT, false)))
+#define SPARQ_ACT_PICK(KERNEL, bf16, align, act, gated)                                                                 \
+    ((act) == SPARQ_ACT_IDENTITY ? SPARQ_ACT_PICK_G(KERNEL, bf16, align, SPARQ_ACT_IDENTITY, gated)                     \
+     : (act) == SPARQ_ACT_RELU ? SPARQ_ACT_PICK_G(KERNEL, bf16, align, SPARQ_ACT_RELU, gated)                           \
+     : (act) == SPARQ_ACT_SILU ? SPARQ_ACT_PICK_G(KERNEL, bf16, align, SPARQ_ACT_SILU, gated)                           \
+                               : SPARQ_ACT_PICK_G(KERNEL, bf16, align, SPARQ_ACT_GELU, gated))
+
+extern "C" int sparq_act_forward_mx8(const void *x, const void *up, int dtype, int64_t rows, int64_t cols, int64_t ldx, int act,
+                                     void *y, int64_t ldy, int8_t *codes, uint8_t *scales, int8_t *up_codes, uint8_t *up_scales, void *stream)
+{
+    int rc = check_act(dtype, act, rows, cols);
+    if (rc != SPARQ_OK || rows == 0 || cols == 0) return rc;
+    if (!x || !y || !codes || !scales) return set_error(SPARQ_ERR_INVALID_ARG, "x/y/codes/scales pointer is NULL");
+    if (!up != !up_codes || !up != !up_scales) return set_error(SPARQ_ERR_INVALID_ARG, "up, up_codes and up_scales come together");
+    rc = check_pitches(dtype, rows, cols, ldx, ldy, (uintptr_t)x | (uintptr_t)up | (uintptr_t)y,
+                       (uintptr_t)codes | (uintptr_t)scales | (uintptr_t)up_codes | (uintptr_t)up_scales);
+    if (rc != SPARQ_OK) return rc;
+    const bool bf16 = dtype == SPARQ_DTYPE_BF16;
+    const int width = bf16 ? 2 : 4;
+    const int align = min_align(min_align(run_align(x, ldx, width), run_align(y, ldy, width)), up ? run_align(up, ldx, width) : 32);
+    const ActForward g = {x, up, rows, cols, ldx, ldy, 2 * mx_scale_cols(SPARQ_MXINT8, cols), y, codes, up_codes, scales, up_scales};
+    int blocks = 0;
+    if ((rc = run_grid(rows * g.per_row, &blocks)) != SPARQ_OK) return rc;
+    const auto kernel = SPARQ_ACT_PICK(act_forward_mx8_kernel, bf16, align, act, up != nullptr);
+    const cudaError_t e = launch_overlapped(kernel, blocks, kRunThreads, 0, (cudaStream_t)stream, g);
+    return e == cudaSuccess ? SPARQ_OK : cuda_error(e, "act_forward_mx8_kernel launch");
+}
+
+extern "C" int sparq_act_backward_mx8(const void *dy, int dtype, int64_t rows, int64_t cols, int64_t lddy, int act,
+                                      const int8_t *codes, const uint8_t *scales, const int8_t *up_codes, const uint8_t *up_scales,
+                                      void *dx, void *dup, int64_t lddx, void *stream)
+{
+    int rc = check_act(dtype, act, rows, cols);
+    if (rc != SPARQ_OK || rows == 0 || cols == 0) return rc;
+    if (!dy || !dx || !codes || !scales) return set_error(SPARQ_ERR_INVALID_ARG, "dy/dx/codes/scales pointer is NULL");
+    if (!dup != !up_codes || !dup != !up_scales) return set_error(SPARQ_ERR_INVALID_ARG, "dup, up_codes and up_scales come together");
+    rc = check_pitches(dtype, rows, cols, lddy, lddx, (uintptr_t)dy | (uintptr_t)dx | (uintptr_t)dup,
+                       (uintptr_t)codes | (uintptr_t)scales | (uintptr_t)up_codes | (uintptr_t)up_scales);
+    if (rc != SPARQ_OK) return rc;
+    const bool bf16 = dtype == SPARQ_DTYPE_BF16;
+    const int width = bf16 ? 2 : 4;
+    const int align = min_align(min_align(run_align(dy, lddy, width), run_align(dx, lddx, width)), dup ? run_align(dup, lddx, width) : 32);
+    const ActBackward g = {dy, codes, up_codes, scales, up_scales, rows, cols, lddy, lddx, (cols + 15) / 16, dx, dup};
+    int blocks = 0;
+    if ((rc = run_grid(rows * g.per_row, &blocks)) != SPARQ_OK) return rc;
+    const auto kernel = SPARQ_ACT_PICK(act_backward_mx8_kernel, bf16, align, act, dup != nullptr);
+    const cudaError_t e = launch_overlapped(kernel, blocks, kRunThreads, 0, (cudaStream_t)stream, g);
+    return e == cudaSuccess ? SPARQ_OK : cuda_error(e, "act_backward_mx8_kernel launch");
+}

@@ -1,0 +1,116 @@
+// Tensor-core instructions of the microscaled contractions: block-scaled 4-bit products (kind::mxf4, kind::mxf4nvf4)
+// with their scales in tensor memory, and bf16 products of operands that lie along the output axes.
+#pragma once
+
+#include "sparq_gemm_kernel.cuh"
+#include "sparq_gemm_small_kernel.cuh"
+#include "sparq_mx.cuh"
+
+namespace sparq {
+
+constexpr int kMxBK = 128;               // bytes of a row per reduction step: 256 4-bit elements, four MMAs of 64
+constexpr int kMxSteps = 4;
+constexpr int kScaleTile = 512;          // 128 rows x 4 scales
+// Scale tiles of 128 rows per reduction step.
+__host__ __device__ constexpr int scale_tiles(bool nv) { return nv ? 4 : 2; }
+
+// Scales of 128 rows from shared memory (32 rows of 16 bytes, 8-row groups back to back) into four columns of
+// tensor memory, the same in every lane quarter.
+__device__ __forceinline__ uint64_t scale_desc(uint32_t saddr)
+{
+    return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(128 >> 4) << 32) | ((uint64_t)1 << 46);
+}
+__device__ __forceinline__ void tc_copy_scales(uint32_t taddr, uint64_t desc)
+{
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" :: "r"(taddr), "l"(desc) : "memory");
+}
+
+// Instruction descriptor of a block-scaled product of e2m1 operands; MXFP4 (e8m0 scales) uses the bytes sf, sf + 1 of each
+// scale word, NVFP4 all four.
+__device__ __forceinline__ constexpr uint32_t make_idesc_f4(int n, int m, bool nv, uint32_t sf)
+{
+    return (sf << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((nv ? 0u : 1u) << 23) | ((uint32_t)(m >> 4) << 24) | (sf << 29);
+}
+
+// D[tmem] (+)= (A * scales) (B * scales), 64 elements of the reduction.
+template <bool NV>
+__device__ __forceinline__ void tc_mma_f4(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate)
+{
+    if (NV)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+            :: "r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+            :: "r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+}
+
+// bf16 operands whose rows run along the reduction axis in memory (MN-major): 64 elements of the output axis are a 128-byte
+// row, swizzled; 8 reduction steps are 1024 bytes, the next 64 elements `block` bytes further.
+__device__ __forceinline__ uint64_t mn_major_desc(uint32_t saddr, uint32_t block)
+{
+    return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(block >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | (2ull << 61);
+}
+__device__ __forceinline__ constexpr uint32_t make_idesc_bf16_mn(int n, int m)
+{
+    return (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+__device__ __forceinline__ void tc_mma_bf16(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        :: "r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void tc_commit(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
+}
+
+// 16 columns of each lane's row.
+__device__ __forceinline__ void tmem_ld_32x16_issue(uint32_t taddr, uint32_t (&r)[32])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr) : "memory");
+}
+
+// Contiguous bytes (16-byte aligned at both ends) into shared memory.
+__device__ __forceinline__ void tma_load_bytes(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 :: "r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+
+__host__ __device__ constexpr int tmem_columns(int want) { return want <= 32 ? 32 : want <= 64 ? 64 : want <= 128 ? 128 : want <= 256 ? 256 : 512; }
+
+// Barriers of a CTA, in shared memory.
+struct MxBars {
+    uint64_t full[kMaxStages], empty[kMaxStages], xf[kMaxStages], acc[2], freed[2], recv;
+};
+
+// One CTA's view of its work; the roles of its warps.
+struct MxCta {
+    uint32_t smem, bars, tmem;          // operand ring (1024-byte aligned), MxBars, accumulator
+    volatile uint32_t *abort_flag;
+    int warp, lane, S, rank, steps;
+    uint32_t split;
+    __device__ uint32_t full_bar(int s) const { return bars + (uint32_t)s * 8u; }
+    __device__ uint32_t empty_bar(int s) const { return bars + (uint32_t)(kMaxStages + s) * 8u; }
+    __device__ uint32_t xf_bar(int s) const { return bars + (uint32_t)(2 * kMaxStages + s) * 8u; }
+    __device__ uint32_t acc_bar(int i = 0) const { return bars + (uint32_t)(3 * kMaxStages + i) * 8u; }
+    __device__ uint32_t freed_bar(int i) const { return bars + (uint32_t)(3 * kMaxStages + 2 + i) * 8u; }
+    __device__ uint32_t recv_bar() const { return bars + (uint32_t)(3 * kMaxStages + 4) * 8u; }
+};
+
+__device__ __forceinline__ void mx_wait_landed(const MxCta &c, unsigned int *status, long long limit)
+{
+    mbar_wait(c.recv_bar(), 0, c.abort_flag, status, limit, true);
+}
+
+}  // namespace sparq

@@ -1,0 +1,96 @@
+// Host side of sparq_gemm_mxf4: validation, choice of form, launch.
+#include "sparq_mxf4_small_kernel.cuh"
+
+namespace sparq {
+
+namespace {
+
+constexpr int kMxMaxDynSmem = 232448 - 4096;
+
+template <int BN, bool NV>
+cudaError_t launch_small(const CUtensorMap &map_b, const CUtensorMap &map_a, MxGemmArgs &g, int64_t grid, cudaStream_t st)
+{
+    auto kernel = sparq_mxf4_small_kernel<BN, NV>;
+    static bool attr_set[64] = {};   // per device ordinal
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= 64 || !attr_set[dev]) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMxMaxDynSmem);
+        if (e != cudaSuccess) return e;
+        if (dev >= 0 && dev < 64) attr_set[dev] = true;
+    }
+    const int recv = mx_recv_bytes(mx_own_groups(g.M < BN ? g.M : BN, g.split), g.split), stage = mx_small_stage(BN, NV);
+    const int steps = (g.k_blocks + g.split - 1) / g.split, fit = (kMxMaxDynSmem - 1024 - recv) / stage;
+    g.stages = steps < fit ? steps : fit;
+    if (g.stages > kMaxStages) g.stages = kMaxStages;
+    return launch_overlapped_cluster(kernel, (int)grid, g.split, kMxSmallThreads, 1024 + g.stages * stage + recv, st, map_b, map_a, g);
+}
+
+template <int BN>
+cudaError_t launch_small_of(bool nv, const CUtensorMap &map_b, const CUtensorMap &map_a, MxGemmArgs &g, int64_t grid, cudaStream_t st)
+{
+    return nv ? launch_small<BN, true>(map_b, map_a, g, grid, st) : launch_small<BN, false>(map_b, map_a, g, grid, st);
+}
+
+}  // namespace
+
+}  // namespace sparq
+
+using namespace sparq;
+
+extern "C" int sparq_gemm_mxf4(const void *A, const uint8_t *A_scales, const void *B, const uint8_t *B_scales,
+                               int64_t M, int64_t N, int64_t K, int format, const sparq_mx_epilogue *e, void *stream)
+{
+    int rc = check_mx_format(format, true);
+    if (rc != SPARQ_OK) return rc;
+    if (!e) return set_error(SPARQ_ERR_INVALID_ARG, "sparq_mx_epilogue is NULL");
+    if ((rc = check_mx_max(format, e->a_max, "a_max")) != SPARQ_OK || (rc = check_mx_max(format, e->b_max, "b_max")) != SPARQ_OK) return rc;
+    if (M < 0 || N < 0 || K < 0) return set_error(SPARQ_ERR_INVALID_ARG, "negative dimension");
+    if (!e->f32_out && !e->bf16_out) return set_error(SPARQ_ERR_INVALID_ARG, "no output requested (f32_out and bf16_out are both NULL)");
+    if (M == 0 || N == 0) return SPARQ_OK;
+    if (K == 0) return set_error(SPARQ_ERR_INVALID_ARG, "K is 0");
+    if (!A || !A_scales || !B || !B_scales) return set_error(SPARQ_ERR_INVALID_ARG, "A/A_scales/B/B_scales pointer is NULL");
+    const int64_t most = INT64_C(2147483647) - 255;
+    if (M >= most || N >= most || K >= most) return set_error(SPARQ_ERR_UNSUPPORTED, "M, N and K must be below 2^31 - 256");
+    if (((uintptr_t)A | (uintptr_t)A_scales | (uintptr_t)B | (uintptr_t)B_scales) & 15u)
+        return set_error(SPARQ_ERR_UNSUPPORTED, "codes and scales must be 16-byte aligned");
+    if (((uintptr_t)e->f32_out & 3u) || ((uintptr_t)e->bf16_out & 1u) || ((uintptr_t)e->bias & 3u))
+        return set_error(SPARQ_ERR_UNSUPPORTED, "outputs and bias must be aligned to their elements");
+    int sms = 0;
+    if ((rc = device_info(&sms)) != SPARQ_OK) return rc;
+
+    const bool nv = format == SPARQ_NVFP4;
+    MxGemmArgs g = {};
+    g.M = M;
+    g.N = N;
+    g.k_mmas = (int)((mx_padded(K) + 63) / 64);
+    g.k_blocks = (g.k_mmas + kMxSteps - 1) / kMxSteps;
+    g.scale_tiles = (int)(mx_scale_cols(format, K) / 4);
+    g.a_scales = A_scales;
+    g.b_scales = B_scales;
+    g.a_max = e->a_max;
+    g.b_max = e->b_max;
+    g.bias = e->bias;
+    g.relu = e->relu;
+    g.f32_out = e->f32_out;
+    g.bf16_out = (uint16_t *)e->bf16_out;
+    g.wait_limit = kWaitLimitCycles;
+    if ((rc = get_status_word(&g.status)) != SPARQ_OK) return rc;
+
+    const int64_t pitch = mx_code_pitch(format, K);
+    const int bn = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
+    const int64_t tiles = (M + bn - 1) / bn * ((N + 127) / 128);
+    g.split = 1;
+    while (g.split < 8 && tiles * g.split * 2 <= sms && g.k_blocks >= 2 * g.split) g.split *= 2;
+    if (tiles * g.split > INT64_C(2147483647)) return set_error(SPARQ_ERR_UNSUPPORTED, "more than 2^31 tiles");
+    CUtensorMap map_a, map_b;
+    if ((rc = encode_matrix(&map_a, CU_TENSOR_MAP_DATA_TYPE_UINT8, A, pitch, M, pitch, kMxBK, bn, CU_TENSOR_MAP_SWIZZLE_128B)) != SPARQ_OK) return rc;
+    if ((rc = encode_matrix(&map_b, CU_TENSOR_MAP_DATA_TYPE_UINT8, B, pitch, N, pitch, kMxBK, 128, CU_TENSOR_MAP_SWIZZLE_128B)) != SPARQ_OK) return rc;
+    cudaStream_t st = (cudaStream_t)stream;
+    const int64_t grid = tiles * g.split;
+    const cudaError_t ce = bn == 16 ? launch_small_of<16>(nv, map_b, map_a, g, grid, st)
+                         : bn == 32 ? launch_small_of<32>(nv, map_b, map_a, g, grid, st)
+                         : bn == 64 ? launch_small_of<64>(nv, map_b, map_a, g, grid, st) : launch_small_of<128>(nv, map_b, map_a, g, grid, st);
+    return ce == cudaSuccess ? SPARQ_OK : cuda_error(ce, "sparq_mxf4_small_kernel launch");
+}

@@ -139,6 +139,7 @@ const char *dtype_text(at::ScalarType t)
     case at::kChar: return "torch.int8";
     case at::kInt: return "torch.int32";
     case at::kFloat: return "torch.float32";
+    case at::kBFloat16: return "torch.bfloat16";
     default: return "another dtype";
     }
 }
@@ -428,6 +429,178 @@ SPARQ_PY(py_gemm_sparse24)
     });
 }
 
+// ---- microscaled formats ----
+
+// A matrix of float32 / bfloat16 whose rows are contiguous; its leading dimension.
+const void *float_rows(const Tensor &t, const char *name, int *dtype, int64_t *ld)
+{
+    const bool bf16 = t.scalar_type() == at::kBFloat16;
+    if (!t.is_cuda() || !(bf16 || t.scalar_type() == at::kFloat)) fail("%s must be a CUDA tensor of float32 or bfloat16", name);
+    if (t.dim() != 2) fail("%s must be a matrix", name);
+    if (t.size(1) > 1 && t.stride(1) != 1) fail("%s must have contiguous rows", name);
+    *dtype = bf16 ? SPARQ_DTYPE_BF16 : SPARQ_DTYPE_F32;
+    *ld = t.size(0) > 1 ? t.stride(0) : t.size(1);
+    return t.data_ptr();
+}
+
+// The same shape, type and leading dimension as another matrix.
+const void *float_rows_like(const Tensor &t, const char *name, const Tensor &as, int dtype, int64_t ld)
+{
+    int dt;
+    int64_t l;
+    const void *p = float_rows(t, name, &dt, &l);
+    if (t.size(0) != as.size(0) || t.size(1) != as.size(1) || dt != dtype) fail("%s has another shape or dtype than its partner", name);
+    if (ld >= 0 && l != ld) fail("%s has another leading dimension than its partner", name);
+    return p;
+}
+
+// Codes and scales of a rows x cols tensor; nullptr for None.
+void *mx_codes(const Tensor *t, const char *name, int format, int64_t rows, int64_t cols)
+{
+    if (!t) return nullptr;
+    const int64_t want = sparq_mx_code_bytes(format, rows, cols);
+    if (want >= 0 && t->numel() < want) fail("%s is smaller than sparq_mx_code_bytes says", name);
+    return format == SPARQ_MXINT8 ? (void *)data<int8_t>(t, at::kChar, name) : (void *)data<uint8_t>(t, at::kByte, name);
+}
+uint8_t *mx_scales(const Tensor *t, const char *name, int format, int64_t rows, int64_t cols)
+{
+    if (!t) return nullptr;
+    const int64_t want = sparq_mx_scale_bytes(format, rows, cols);
+    if (want >= 0 && t->numel() < want) fail("%s is smaller than sparq_mx_scale_bytes says", name);
+    return data<uint8_t>(t, at::kByte, name);
+}
+float *one_float(const Tensor *t, const char *name)
+{
+    if (t && t->numel() < 1) fail("%s is empty", name);
+    return data<float>(t, at::kFloat, name);
+}
+
+// (values, format, codes, scales, max_dev, stream); `values` is the input or, decoding, the output
+PyObject *mx_codec_call(PyObject *const *args, Py_ssize_t nargs, bool encode)
+{
+    return guarded([&] {
+        Args a(args, nargs, 6);
+        const char *name = encode ? "x" : "out";
+        const Tensor &x = a.tensor(name);
+        const int format = (int)a.integer();
+        const Tensor &c = a.tensor("codes"), &s = a.tensor("scales"), *m = a.opt("max_dev");
+        int dt;
+        int64_t ld;
+        void *px = (void *)float_rows(x, name, &dt, &ld);
+        const int64_t rows = x.size(0), cols = x.size(1);
+        void *pc = mx_codes(&c, "codes", format, rows, cols);
+        uint8_t *ps = mx_scales(&s, "scales", format, rows, cols);
+        const float *pm = one_float(m, "max_dev");
+        void *st = a.stream();
+        return call([&] {
+            return encode ? sparq_quantize_mx(px, dt, rows, cols, ld, format, pm, pc, ps, st)
+                          : sparq_dequantize_mx(pc, ps, rows, cols, format, pm, px, dt, ld, st);
+        });
+    });
+}
+SPARQ_PY(py_quantize_mx) { return mx_codec_call(args, nargs, true); }
+SPARQ_PY(py_dequantize_mx) { return mx_codec_call(args, nargs, false); }
+
+// (A, A_scales, B, B_scales, format, a_max, b_max, bias, relu, f32_out, bf16_out, stream)
+SPARQ_PY(py_gemm_mxf4)
+{
+    return guarded([&] {
+        Args a(args, nargs, 12);
+        const Tensor &A = a.tensor("A"), &As = a.tensor("A_scales"), &B = a.tensor("B"), &Bs = a.tensor("B_scales");
+        const int format = (int)a.integer();
+        if (A.dim() != 2 || B.dim() != 2) fail("%s must be matrices", "A and B");
+        const int64_t M = A.size(0), N = B.size(0), K = 2 * A.size(1);
+        if (2 * B.size(1) != K) fail("%s disagree on K", "A and B");
+        if (K % 32) fail("%s do not have whole blocks of 32 codes", "A and B");
+        sparq_mx_epilogue e = {};
+        e.a_max = one_float(a.opt("a_max"), "a_max");
+        e.b_max = one_float(a.opt("b_max"), "b_max");
+        const Tensor *bias = a.opt("bias");
+        if (bias && bias->numel() < N) fail("%s has fewer than N elements", "bias");
+        e.bias = data<float>(bias, at::kFloat, "bias");
+        e.relu = a.truth();
+        const Tensor *f32 = a.opt("f32_out"), *bf16 = a.opt("bf16_out");
+        if (f32 && f32->numel() < M * N) fail("%s has fewer than M*N elements", "f32_out");
+        if (bf16 && bf16->numel() < M * N) fail("%s has fewer than M*N elements", "bf16_out");
+        e.f32_out = data<float>(f32, at::kFloat, "f32_out");
+        e.bf16_out = data<void>(bf16, at::kBFloat16, "bf16_out");
+        const bool four = format == SPARQ_MXFP4 || format == SPARQ_NVFP4;      // the library refuses others
+        const void *pa = four ? mx_codes(&A, "A", format, M, K) : data<void>(&A, at::kByte, "A");
+        const void *pb = four ? mx_codes(&B, "B", format, N, K) : data<void>(&B, at::kByte, "B");
+        const uint8_t *sa = four ? mx_scales(&As, "A_scales", format, M, K) : nullptr;
+        const uint8_t *sb = four ? mx_scales(&Bs, "B_scales", format, N, K) : nullptr;
+        void *st = a.stream();
+        return call([&] { return sparq_gemm_mxf4(pa, sa, pb, sb, M, N, K, format, &e, st); });
+    });
+}
+
+// (x, act, y, codes, scales, up, up_codes, up_scales, stream)
+SPARQ_PY(py_act_forward_mx8)
+{
+    return guarded([&] {
+        Args a(args, nargs, 9);
+        const Tensor &x = a.tensor("x");
+        const int act = (int)a.integer();
+        const Tensor &y = a.tensor("y"), &c = a.tensor("codes"), &s = a.tensor("scales");
+        const Tensor *up = a.opt("up"), *uc = a.opt("up_codes"), *us = a.opt("up_scales");
+        int dt;
+        int64_t ldx, ldy;
+        const void *px = float_rows(x, "x", &dt, &ldx);
+        void *py = (void *)float_rows_like(y, "y", x, dt, -1);
+        ldy = y.size(0) > 1 ? y.stride(0) : y.size(1);
+        const void *pu = up ? float_rows_like(*up, "up", x, dt, ldx) : nullptr;
+        const int64_t rows = x.size(0), cols = x.size(1);
+        int8_t *pc = (int8_t *)mx_codes(&c, "codes", SPARQ_MXINT8, rows, cols), *puc = (int8_t *)mx_codes(uc, "up_codes", SPARQ_MXINT8, rows, cols);
+        uint8_t *ps = mx_scales(&s, "scales", SPARQ_MXINT8, rows, cols), *pus = mx_scales(us, "up_scales", SPARQ_MXINT8, rows, cols);
+        void *st = a.stream();
+        return call([&] { return sparq_act_forward_mx8(px, pu, dt, rows, cols, ldx, act, py, ldy, pc, ps, puc, pus, st); });
+    });
+}
+
+// (dy, act, codes, scales, dx, up_codes, up_scales, dup, stream)
+SPARQ_PY(py_act_backward_mx8)
+{
+    return guarded([&] {
+        Args a(args, nargs, 9);
+        const Tensor &dy = a.tensor("dy");
+        const int act = (int)a.integer();
+        const Tensor &c = a.tensor("codes"), &s = a.tensor("scales"), &dx = a.tensor("dx");
+        const Tensor *uc = a.opt("up_codes"), *us = a.opt("up_scales"), *dup = a.opt("dup");
+        int dt;
+        int64_t lddy;
+        const void *pdy = float_rows(dy, "dy", &dt, &lddy);
+        void *pdx = (void *)float_rows_like(dx, "dx", dy, dt, -1);
+        const int64_t lddx = dx.size(0) > 1 ? dx.stride(0) : dx.size(1);
+        void *pdup = dup ? (void *)float_rows_like(*dup, "dup", dy, dt, lddx) : nullptr;
+        const int64_t rows = dy.size(0), cols = dy.size(1);
+        const int8_t *pc = (int8_t *)mx_codes(&c, "codes", SPARQ_MXINT8, rows, cols), *puc = (int8_t *)mx_codes(uc, "up_codes", SPARQ_MXINT8, rows, cols);
+        const uint8_t *ps = mx_scales(&s, "scales", SPARQ_MXINT8, rows, cols), *pus = mx_scales(us, "up_scales", SPARQ_MXINT8, rows, cols);
+        void *st = a.stream();
+        return call([&] { return sparq_act_backward_mx8(pdy, dt, rows, cols, lddy, act, pc, ps, puc, pus, pdx, pdup, lddx, st); });
+    });
+}
+
+// (dy, codes, scales, dw, accumulate, stream)
+SPARQ_PY(py_wgrad_mx8)
+{
+    return guarded([&] {
+        Args a(args, nargs, 6);
+        const Tensor &dy = a.tensor("dy"), &c = a.tensor("codes"), &s = a.tensor("scales"), &dw = a.tensor("dw");
+        int dt;
+        int64_t ld;
+        const void *pdy = float_rows(dy, "dy", &dt, &ld);
+        if (dt != SPARQ_DTYPE_BF16) fail("%s must have dtype torch.bfloat16", "dy");
+        if (dw.dim() != 2 || dw.size(0) != dy.size(1)) fail("%s must be a matrix with a row per column of dy", "dw");
+        const int64_t M = dy.size(0), N = dy.size(1), K = dw.size(1);
+        const int8_t *pc = (int8_t *)mx_codes(&c, "codes", SPARQ_MXINT8, M, K);
+        const uint8_t *ps = mx_scales(&s, "scales", SPARQ_MXINT8, M, K);
+        float *pdw = data<float>(&dw, at::kFloat, "dw");
+        const int accumulate = a.truth();
+        void *st = a.stream();
+        return call([&] { return sparq_wgrad_mx8(pdy, ld, pc, ps, M, N, K, accumulate, pdw, st); });
+    });
+}
+
 #define SPARQ_DEF(name, fn) {name, (PyCFunction)(void (*)(void))fn, METH_FASTCALL, nullptr}
 
 PyMethodDef kMethods[] = {
@@ -445,6 +618,12 @@ PyMethodDef kMethods[] = {
     SPARQ_DEF("quantize_weight", py_quantize_weight),
     SPARQ_DEF("expand_activations", py_expand_activations),
     SPARQ_DEF("gemm_sparse24", py_gemm_sparse24),
+    SPARQ_DEF("quantize_mx", py_quantize_mx),
+    SPARQ_DEF("dequantize_mx", py_dequantize_mx),
+    SPARQ_DEF("gemm_mxf4", py_gemm_mxf4),
+    SPARQ_DEF("act_forward_mx8", py_act_forward_mx8),
+    SPARQ_DEF("act_backward_mx8", py_act_backward_mx8),
+    SPARQ_DEF("wgrad_mx8", py_wgrad_mx8),
     {nullptr, nullptr, 0, nullptr},
 };
 

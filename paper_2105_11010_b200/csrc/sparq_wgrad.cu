@@ -1,0 +1,59 @@
+// Host side of sparq_wgrad_mx8: validation, choice of form, launch.
+#include "sparq_wgrad_kernel.cuh"
+
+using namespace sparq;
+
+extern "C" int sparq_wgrad_mx8(const void *dy, int64_t lddy, const int8_t *codes, const uint8_t *scales,
+                               int64_t M, int64_t N, int64_t K, int accumulate, float *dw, void *stream)
+{
+    if (M < 0 || N < 0 || K < 0) return set_error(SPARQ_ERR_INVALID_ARG, "negative dimension");
+    if (N == 0 || K == 0) return SPARQ_OK;
+    if (!dw) return set_error(SPARQ_ERR_INVALID_ARG, "dw is NULL");
+    if ((uintptr_t)dw & 3u) return set_error(SPARQ_ERR_UNSUPPORTED, "dw must be 4-byte aligned");
+    const int64_t most = INT64_C(2147483647) - 255;
+    if (M >= most || N >= most || K >= most) return set_error(SPARQ_ERR_UNSUPPORTED, "M, N and K must be below 2^31 - 256");
+    cudaStream_t st = (cudaStream_t)stream;
+    if (M == 0) {           // a sum over no tokens
+        if (accumulate) return SPARQ_OK;
+        const cudaError_t e = cudaMemsetAsync(dw, 0, (size_t)N * (size_t)K * sizeof(float), st);
+        return e == cudaSuccess ? SPARQ_OK : cuda_error(e, "cudaMemsetAsync(dw)");
+    }
+    if (!dy || !codes || !scales) return set_error(SPARQ_ERR_INVALID_ARG, "dy/codes/scales pointer is NULL");
+    if (M == 1) lddy = round_up64(N, 8);      // a single row has no pitch
+    if (lddy < N) return set_error(SPARQ_ERR_INVALID_ARG, "the leading dimension of dy (%lld) is less than N (%lld)", (long long)lddy, (long long)N);
+    if (lddy % 8 || ((uintptr_t)dy & 15u)) return set_error(SPARQ_ERR_UNSUPPORTED, "dy must be 16-byte aligned and its leading dimension a multiple of 8");
+    if (((uintptr_t)codes | (uintptr_t)scales) & 15u) return set_error(SPARQ_ERR_UNSUPPORTED, "codes and scales must be 16-byte aligned");
+    if (lddy > INT64_C(1) << 38) return set_error(SPARQ_ERR_UNSUPPORTED, "the leading dimension of dy is %lld", (long long)lddy);
+    int sms = 0, rc = device_info(&sms);
+    if (rc != SPARQ_OK) return rc;
+
+    WgradArgs g = {};
+    g.M = M;
+    g.N = N;
+    g.K = K;
+    g.blocks = (int)((M + kWgTokens - 1) / kWgTokens);
+    g.accumulate = accumulate != 0;
+    g.dw = dw;
+    g.wait_limit = kWaitLimitCycles;
+    if ((rc = get_status_word(&g.status)) != SPARQ_OK) return rc;
+    const int64_t tiles = (N + 127) / 128 * ((K + kWgBN - 1) / kWgBN);
+    g.split = 1;
+    while (g.split < 8 && tiles * g.split * 2 <= sms && g.blocks >= 4 * g.split) g.split *= 2;
+    g.stages = kWgStages;
+    if (tiles * g.split > INT64_C(2147483647)) return set_error(SPARQ_ERR_UNSUPPORTED, "more than 2^31 tiles");
+    CUtensorMap map_dy, map_codes, map_scales;
+    const int64_t pitch = mx_code_pitch(SPARQ_MXINT8, K), spitch = mx_scale_cols(SPARQ_MXINT8, K);
+    if ((rc = encode_matrix(&map_dy, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, dy, N, M, lddy * 2, 64, kWgTokens, CU_TENSOR_MAP_SWIZZLE_128B)) != SPARQ_OK) return rc;
+    if ((rc = encode_matrix(&map_codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, pitch, M, pitch, kWgBN, kWgTokens, CU_TENSOR_MAP_SWIZZLE_NONE)) != SPARQ_OK) return rc;
+    if ((rc = encode_matrix(&map_scales, CU_TENSOR_MAP_DATA_TYPE_UINT8, scales, spitch, M, spitch, 16, kWgTokens, CU_TENSOR_MAP_SWIZZLE_NONE)) != SPARQ_OK) return rc;
+    static bool attr_set[64] = {};   // per device ordinal
+    const int smem = 1024 + kWgStages * kWgStage;
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess && (dev < 0 || dev >= 64 || !attr_set[dev])) {
+        e = cudaFuncSetAttribute(sparq_wgrad_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e == cudaSuccess && dev >= 0 && dev < 64) attr_set[dev] = true;
+    }
+    if (e == cudaSuccess) e = launch_overlapped_cluster(sparq_wgrad_small_kernel, (int)(tiles * g.split), g.split, kWgThreads, smem, st, map_dy, map_codes, map_scales, g);
+    return e == cudaSuccess ? SPARQ_OK : cuda_error(e, "sparq_wgrad_small_kernel launch");
+}
