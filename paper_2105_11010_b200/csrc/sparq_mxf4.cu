@@ -1,5 +1,5 @@
 // Host side of sparq_gemm_mxf4: validation, choice of form, launch.
-#include "sparq_mxf4_small_kernel.cuh"
+#include "sparq_mxf4_kernel.cuh"
 
 namespace sparq {
 
@@ -31,6 +31,29 @@ template <int BN>
 cudaError_t launch_small_of(bool nv, const CUtensorMap &map_b, const CUtensorMap &map_a, MxGemmArgs &g, int64_t grid, cudaStream_t st)
 {
     return nv ? launch_small<BN, true>(map_b, map_a, g, grid, st) : launch_small<BN, false>(map_b, map_a, g, grid, st);
+}
+
+template <bool NV>
+cudaError_t launch_pair(const CUtensorMap &map_a, const CUtensorMap &map_b, const CUtensorMap &map_sa, const CUtensorMap &map_sb, const MxPairArgs &p, cudaStream_t st)
+{
+    auto kernel = sparq_mxf4_kernel<NV>;
+    const int smem = 1024 + pair_stages(NV) * pair_stage_room(NV);
+    static bool attr_set[64] = {};   // per device ordinal
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= 64 || !attr_set[dev]) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != cudaSuccess) return e;
+        if (dev >= 0 && dev < 64) attr_set[dev] = true;
+    }
+    return launch_overlapped_cluster(kernel, 2 * p.pairs, 2, kPairThreads, smem, st, map_a, map_b, map_sa, map_sb, p);
+}
+
+// A matrix's scale tiles, as rows of 128 words.
+int encode_scales(CUtensorMap *map, const uint8_t *scales, int64_t tiles, bool nv)
+{
+    return encode_matrix(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, scales, 128, tiles, kScaleTile, 128, scale_tiles(nv), CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
 }  // namespace
@@ -79,6 +102,20 @@ extern "C" int sparq_gemm_mxf4(const void *A, const uint8_t *A_scales, const voi
     if ((rc = get_status_word(&g.status)) != SPARQ_OK) return rc;
 
     const int64_t pitch = mx_code_pitch(format, K);
+    cudaStream_t st = (cudaStream_t)stream;
+    const int64_t m_tiles = (M + kPairTile - 1) / kPairTile, n_tiles = (N + kPairTile - 1) / kPairTile;
+    if (m_tiles * n_tiles * 2 >= sms && m_tiles * n_tiles <= INT64_C(1) << 30 && m_tiles * 2 * g.scale_tiles < most && n_tiles * 2 * g.scale_tiles < most) {
+        MxPairArgs p = {g, (int)m_tiles, (int)n_tiles, 0};
+        p.pairs = (int)(m_tiles * n_tiles < sms / 2 ? m_tiles * n_tiles : sms / 2);
+        CUtensorMap map_a, map_b, map_sa, map_sb;
+        if ((rc = encode_matrix(&map_a, CU_TENSOR_MAP_DATA_TYPE_UINT8, A, pitch, M, pitch, kMxBK, 128, CU_TENSOR_MAP_SWIZZLE_128B)) != SPARQ_OK ||
+            (rc = encode_matrix(&map_b, CU_TENSOR_MAP_DATA_TYPE_UINT8, B, pitch, N, pitch, kMxBK, 128, CU_TENSOR_MAP_SWIZZLE_128B)) != SPARQ_OK ||
+            (rc = encode_scales(&map_sa, A_scales, (M + 127) / 128 * g.scale_tiles, nv)) != SPARQ_OK ||
+            (rc = encode_scales(&map_sb, B_scales, (N + 127) / 128 * g.scale_tiles, nv)) != SPARQ_OK)
+            return rc;
+        const cudaError_t ce = nv ? launch_pair<true>(map_a, map_b, map_sa, map_sb, p, st) : launch_pair<false>(map_a, map_b, map_sa, map_sb, p, st);
+        return ce == cudaSuccess ? SPARQ_OK : cuda_error(ce, "sparq_mxf4_kernel launch");
+    }
     const int bn = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
     const int64_t tiles = (M + bn - 1) / bn * ((N + 127) / 128);
     g.split = 1;
@@ -87,7 +124,6 @@ extern "C" int sparq_gemm_mxf4(const void *A, const uint8_t *A_scales, const voi
     CUtensorMap map_a, map_b;
     if ((rc = encode_matrix(&map_a, CU_TENSOR_MAP_DATA_TYPE_UINT8, A, pitch, M, pitch, kMxBK, bn, CU_TENSOR_MAP_SWIZZLE_128B)) != SPARQ_OK) return rc;
     if ((rc = encode_matrix(&map_b, CU_TENSOR_MAP_DATA_TYPE_UINT8, B, pitch, N, pitch, kMxBK, 128, CU_TENSOR_MAP_SWIZZLE_128B)) != SPARQ_OK) return rc;
-    cudaStream_t st = (cudaStream_t)stream;
     const int64_t grid = tiles * g.split;
     const cudaError_t ce = bn == 16 ? launch_small_of<16>(nv, map_b, map_a, g, grid, st)
                          : bn == 32 ? launch_small_of<32>(nv, map_b, map_a, g, grid, st)
