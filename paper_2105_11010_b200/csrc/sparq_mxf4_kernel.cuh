@@ -131,23 +131,28 @@ struct Mxf4Pair : MxCta {
         __syncwarp();
     }
 
-    // 16 columns of a row.
-    __device__ void put(const MxGemmArgs &g, const uint32_t *v, int64_t m, int64_t n, float alpha, bool vec_f, bool vec_h) const
+    // 16 columns of a row.  WHOLE: all of them exist, outputs and bias on 32-byte boundaries.
+    template <bool WHOLE>
+    __device__ void put(const MxGemmArgs &g, const uint32_t *v, int64_t m, int64_t n, float alpha) const
     {
-        if (m >= g.M || n >= g.N) return;
-        const int cols = g.N - n < 16 ? (int)(g.N - n) : 16;
+        if (m >= g.M || (!WHOLE && n >= g.N)) return;
+        const int cols = WHOLE || g.N - n >= 16 ? 16 : (int)(g.N - n);
         float y[16];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) y[j] = mx_finish(__uint_as_float(v[j]), alpha, g.bias && j < cols ? __ldg(g.bias + n + j) : 0.0f, g.relu);
+        for (int j = 0; j < 16; ++j) y[j] = __fmul_rn(__uint_as_float(v[j]), alpha);
+        if (g.bias) {
+            float b[16];
+            load_run<false, WHOLE ? 32 : 0>(b, g.bias + n, cols);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) y[j] = __fadd_rn(y[j], b[j]);
+        }
+        if (g.relu) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) y[j] = y[j] > 0.0f ? y[j] : 0.0f;
+        }
         const int64_t at = m * g.N + n;
-        if (g.f32_out) {
-            if (vec_f) store_run<false, 32>(g.f32_out + at, y, cols);
-            else store_run<false, 0>(g.f32_out + at, y, cols);
-        }
-        if (g.bf16_out) {
-            if (vec_h) store_run<true, 32>(g.bf16_out + at, y, cols);
-            else store_run<true, 0>(g.bf16_out + at, y, cols);
-        }
+        if (g.f32_out) store_run<false, WHOLE ? 32 : 0>(g.f32_out + at, y, cols);
+        if (g.bf16_out) store_run<true, WHOLE ? 32 : 0>(g.bf16_out + at, y, cols);
     }
 
     __device__ void finish(const MxPairArgs &p) const
@@ -155,8 +160,8 @@ struct Mxf4Pair : MxCta {
         const MxGemmArgs &g = p.g;
         const int quarter = warp & 3, half = (warp - 2) >> 2;
         const float alpha = mx_alpha(g);
-        const bool vec_f = (g.N & 7) == 0 && (reinterpret_cast<uintptr_t>(g.f32_out) & 31u) == 0;
-        const bool vec_h = (g.N & 15) == 0 && (reinterpret_cast<uintptr_t>(g.bf16_out) & 31u) == 0;
+        const bool aligned = (g.N & (g.bf16_out ? 15 : 7)) == 0 &&
+                             ((reinterpret_cast<uintptr_t>(g.f32_out) | reinterpret_cast<uintptr_t>(g.bf16_out) | reinterpret_cast<uintptr_t>(g.bias)) & 31u) == 0;
         const uint32_t freed = map_to_rank(freed_bar(0), 0);
         int i = 0;
         for (int t = pair; t < tiles; t += p.pairs, ++i) {
@@ -166,6 +171,7 @@ struct Mxf4Pair : MxCta {
             mbar_wait(acc_bar(i & 1), (uint32_t)(i >> 1) & 1u, abort_flag, g.status, g.wait_limit);
             tc_fence_after();
             const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (i & 1) * kPairSecond;
+            const bool whole = aligned && n0 + kPairTile <= g.N;
             // run r of 16 columns; the ones that the next tile's accumulator shares come first: 13, 14, 15 of the even tiles, 0, 1, 2 of the odd
             auto run_of = [&](int q) { return (i & 1) ? q : q < 3 ? 13 + q : q - 3; };
 #pragma unroll 1
@@ -180,8 +186,13 @@ struct Mxf4Pair : MxCta {
                     __syncwarp();
                     if (lane == 0) mbar_arrive_remote(freed);
                 }
-                put(g, va, m, n0 + ra * 16, alpha, vec_f, vec_h);
-                put(g, vb, m, n0 + rb * 16, alpha, vec_f, vec_h);
+                if (whole) {
+                    put<true>(g, va, m, n0 + ra * 16, alpha);
+                    put<true>(g, vb, m, n0 + rb * 16, alpha);
+                } else {
+                    put<false>(g, va, m, n0 + ra * 16, alpha);
+                    put<false>(g, vb, m, n0 + rb * 16, alpha);
+                }
             }
         }
         tc_fence_before();
