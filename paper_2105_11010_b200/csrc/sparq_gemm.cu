@@ -101,6 +101,28 @@ int encode_matrix(CUtensorMap *map, CUtensorMapDataType type, const void *ptr, i
     return SPARQ_OK;
 }
 
+// Tiles of 128 x 4 scale bytes (sparq_mx.cuh) as rows of 128 words: `tiles` to a row block, `blocks` row blocks, read
+// box_tiles x box_blocks at a time.
+int encode_scale_tiles(CUtensorMap *map, const void *ptr, int64_t tiles, int64_t blocks, int box_tiles, int box_blocks)
+{
+    static EncodeTiledFn fn = nullptr;
+    if (!fn) {
+        int rc = driver_fn("cuTensorMapEncodeTiled", (void **)&fn);
+        if (rc != SPARQ_OK) return rc;
+    }
+    const MapKey key = {{7, (uint64_t)(uintptr_t)ptr, (uint64_t)tiles, (uint64_t)blocks, (uint64_t)box_tiles, (uint64_t)box_blocks}};
+    if (map_lookup(key, map)) return SPARQ_OK;
+    cuuint64_t dims[3] = {128, (cuuint64_t)tiles, (cuuint64_t)blocks};
+    cuuint64_t strides[2] = {512, (cuuint64_t)tiles * 512};
+    cuuint32_t box[3] = {128, (cuuint32_t)box_tiles, (cuuint32_t)box_blocks};
+    cuuint32_t estr[3] = {1, 1, 1};
+    CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, const_cast<void *>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                    CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return set_error(SPARQ_ERR_CUDA, "cuTensorMapEncodeTiled (scales) failed with CUresult %d", (int)r);
+    map_store(key, *map);
+    return SPARQ_OK;
+}
+
 // 2-D K-contiguous matrix [rows][K] with row pitch ld bytes; box = bk x box_rows.
 static int encode_2d(CUtensorMap *map, const void *ptr, int64_t K, int64_t rows, int64_t ld, int bk, int box_rows)
 {

@@ -64,6 +64,7 @@ constexpr long long kWaitLimitCycles = 2000000000LL;
 int device_info(int *sms);
 int encode_matrix(CUtensorMap *map, CUtensorMapDataType type, const void *ptr, int64_t inner, int64_t rows, int64_t pitch, int box_inner,
                   int box_rows, CUtensorMapSwizzle swizzle);
+int encode_scale_tiles(CUtensorMap *map, const void *ptr, int64_t tiles, int64_t blocks, int box_tiles, int box_blocks);
 
 struct GemmArgs {
     // problem

@@ -98,6 +98,11 @@ __device__ __forceinline__ void tma_load_pair_2d(uint32_t dst, const CUtensorMap
     asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
                  :: "r"(dst), "l"(map), "r"(leader_bar), "r"(x), "r"(y) : "memory");
 }
+__device__ __forceinline__ void tma_load_pair_3d(uint32_t dst, const CUtensorMap *map, uint32_t leader_bar, int x, int y, int z)
+{
+    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                 :: "r"(dst), "l"(map), "r"(leader_bar), "r"(x), "r"(y), "r"(z) : "memory");
+}
 // Arrives on the same barrier of both CTAs once the MMAs before it have retired.
 __device__ __forceinline__ void tc_commit_pair(uint32_t bar)
 {

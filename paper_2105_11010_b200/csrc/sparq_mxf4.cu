@@ -34,10 +34,10 @@ cudaError_t launch_small_of(bool nv, const CUtensorMap &map_b, const CUtensorMap
 }
 
 template <bool NV>
-cudaError_t launch_pair(const CUtensorMap &map_a, const CUtensorMap &map_b, const CUtensorMap &map_sa, const CUtensorMap &map_sb, const MxPairArgs &p, cudaStream_t st)
+cudaError_t launch_pair(const CUtensorMap (&map)[6], const MxPairArgs &p, cudaStream_t st)
 {
     auto kernel = sparq_mxf4_kernel<NV>;
-    const int smem = 1024 + pair_stages(NV) * pair_stage_room(NV);
+    const int smem = pair_smem(NV);
     static bool attr_set[64] = {};   // per device ordinal
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -47,13 +47,7 @@ cudaError_t launch_pair(const CUtensorMap &map_a, const CUtensorMap &map_b, cons
         if (e != cudaSuccess) return e;
         if (dev >= 0 && dev < 64) attr_set[dev] = true;
     }
-    return launch_overlapped_cluster(kernel, 2 * p.pairs, 2, kPairThreads, smem, st, map_a, map_b, map_sa, map_sb, p);
-}
-
-// A matrix's scale tiles, as rows of 128 words.
-int encode_scales(CUtensorMap *map, const uint8_t *scales, int64_t tiles, bool nv)
-{
-    return encode_matrix(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, scales, 128, tiles, kScaleTile, 128, scale_tiles(nv), CU_TENSOR_MAP_SWIZZLE_NONE);
+    return launch_overlapped_cluster(kernel, 2 * p.pairs, 2, kPairThreads, smem, st, map[0], map[1], map[2], map[3], map[4], map[5], p);
 }
 
 }  // namespace
@@ -104,16 +98,21 @@ extern "C" int sparq_gemm_mxf4(const void *A, const uint8_t *A_scales, const voi
     const int64_t pitch = mx_code_pitch(format, K);
     cudaStream_t st = (cudaStream_t)stream;
     const int64_t m_tiles = (M + kPairTile - 1) / kPairTile, n_tiles = (N + kPairTile - 1) / kPairTile;
-    if (m_tiles * n_tiles * 2 >= sms && m_tiles * n_tiles <= INT64_C(1) << 30 && m_tiles * 2 * g.scale_tiles < most && n_tiles * 2 * g.scale_tiles < most) {
-        MxPairArgs p = {g, (int)m_tiles, (int)n_tiles, 0};
+    if (m_tiles * n_tiles >= 16 && m_tiles * n_tiles <= INT64_C(1) << 30) {
+        MxPairArgs p = {g, (int)m_tiles, (int)n_tiles, 0, 0};
         p.pairs = (int)(m_tiles * n_tiles < sms / 2 ? m_tiles * n_tiles : sms / 2);
-        CUtensorMap map_a, map_b, map_sa, map_sb;
-        if ((rc = encode_matrix(&map_a, CU_TENSOR_MAP_DATA_TYPE_UINT8, A, pitch, M, pitch, kMxBK, 128, CU_TENSOR_MAP_SWIZZLE_128B)) != SPARQ_OK ||
-            (rc = encode_matrix(&map_b, CU_TENSOR_MAP_DATA_TYPE_UINT8, B, pitch, N, pitch, kMxBK, 128, CU_TENSOR_MAP_SWIZZLE_128B)) != SPARQ_OK ||
-            (rc = encode_scales(&map_sa, A_scales, (M + 127) / 128 * g.scale_tiles, nv)) != SPARQ_OK ||
-            (rc = encode_scales(&map_sb, B_scales, (N + 127) / 128 * g.scale_tiles, nv)) != SPARQ_OK)
+        p.staged = (N % (e->bf16_out ? 8 : 4)) == 0 && (((uintptr_t)e->f32_out | (uintptr_t)e->bf16_out) & 15u) == 0;
+        CUtensorMap map[6] = {};
+        if ((rc = encode_matrix(&map[0], CU_TENSOR_MAP_DATA_TYPE_UINT8, A, pitch, M, pitch, kMxBK, 128, CU_TENSOR_MAP_SWIZZLE_128B)) != SPARQ_OK ||
+            (rc = encode_matrix(&map[1], CU_TENSOR_MAP_DATA_TYPE_UINT8, B, pitch, N, pitch, kMxBK, 128, CU_TENSOR_MAP_SWIZZLE_128B)) != SPARQ_OK ||
+            (rc = encode_scale_tiles(&map[2], A_scales, g.scale_tiles, (M + 127) / 128, scale_tiles(nv), 1)) != SPARQ_OK ||
+            (rc = encode_scale_tiles(&map[3], B_scales, g.scale_tiles, (N + 127) / 128, scale_tiles(nv), 2)) != SPARQ_OK)
             return rc;
-        const cudaError_t ce = nv ? launch_pair<true>(map_a, map_b, map_sa, map_sb, p, st) : launch_pair<false>(map_a, map_b, map_sa, map_sb, p, st);
+        if (p.staged && e->f32_out &&
+            (rc = encode_matrix(&map[4], CU_TENSOR_MAP_DATA_TYPE_FLOAT32, e->f32_out, N, M, N * 4, 32, 32, CU_TENSOR_MAP_SWIZZLE_128B)) != SPARQ_OK) return rc;
+        if (p.staged && e->bf16_out &&
+            (rc = encode_matrix(&map[5], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, e->bf16_out, N, M, N * 2, 64, 32, CU_TENSOR_MAP_SWIZZLE_128B)) != SPARQ_OK) return rc;
+        const cudaError_t ce = nv ? launch_pair<true>(map, p, st) : launch_pair<false>(map, p, st);
         return ce == cudaSuccess ? SPARQ_OK : cuda_error(ce, "sparq_mxf4_kernel launch");
     }
     const int bn = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;

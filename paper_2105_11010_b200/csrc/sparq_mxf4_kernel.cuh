@@ -11,8 +11,7 @@
 // Tensor memory: 464 columns of accumulators, 48 of scales.  Two accumulators of 256 columns do not fit, so they share 48
 // columns: the epilogue empties those first (columns 208..255), and the next tile's first MMA waits for no more than that.
 //
-// Warps: 0 producer, 1 tensor memory and (leader) MMA issue, 2..9 epilogue (lane quarter warp % 4, every second run of 16
-// columns).
+// Warps: 0 producer of the codes, 10 of the scales, 1 tensor memory and (leader) MMA issue, 2..9 epilogue (lane quarter warp % 4, two spans of 64 columns).
 #pragma once
 
 #include "sparq_mxf4_small_kernel.cuh"
@@ -20,19 +19,23 @@
 namespace sparq {
 
 constexpr int kPairTile = 256;
-constexpr int kPairThreads = 320;
 constexpr int kPairEpiWarps = 8;
+constexpr int kPairScaleWarp = 2 + kPairEpiWarps;
+constexpr int kPairThreads = 32 * (kPairScaleWarp + 1);
 constexpr uint32_t kPairSecond = 208;           // first column of the odd tiles' accumulator
 constexpr uint32_t kPairScales = 464;           // first column of the scales
 
 __host__ __device__ constexpr int pair_stage(bool nv) { return 2 * 128 * kMxBK + 3 * scale_tiles(nv) * kScaleTile; }
 // Stages start on 1024-byte boundaries.
 __host__ __device__ constexpr int pair_stage_room(bool nv) { return (pair_stage(nv) + 1023) / 1024 * 1024; }
-__host__ __device__ constexpr int pair_stages(bool nv) { return (232448 - 4096) / pair_stage_room(nv) < kMaxStages ? (232448 - 4096) / pair_stage_room(nv) : kMaxStages; }
+constexpr int kPairStaging = 32 * 128;          // per epilogue warp: 32 rows of a box
+__host__ __device__ constexpr int pair_stages(bool nv) { return (232448 - 1024 - 512 - kPairEpiWarps * kPairStaging) / pair_stage_room(nv); }
+__host__ __device__ constexpr int pair_smem(bool nv) { return 1024 + pair_stages(nv) * pair_stage_room(nv) + kPairEpiWarps * kPairStaging; }
 
 struct MxPairArgs {
     MxGemmArgs g;
     int m_tiles, n_tiles, pairs;
+    int staged;                 // outputs go out through shared memory, in boxes
 };
 
 // Tile t in an order that keeps eight rows of tiles together: their operands and the column's stay in L2.
@@ -50,11 +53,15 @@ struct Mxf4Pair : MxCta {
     static constexpr int kBytes = pair_stage(NV), kRoom = pair_stage_room(NV), kStages = pair_stages(NV);
     int tiles, pair;
 
-    __device__ void produce(const CUtensorMap &map_a, const CUtensorMap &map_b, const CUtensorMap &map_sa, const CUtensorMap &map_sb, const MxPairArgs &p) const
+    // Two producers, one for the codes and one for the scales, on the same barriers: one thread that issued all four copies of a
+    // step took longer than the step's MMAs (16 pairs, K 32768: 0.36 us a step, 0.28 without the scales' copies).
+    template <bool CODES>
+    __device__ void produce(const CUtensorMap &map_a, const CUtensorMap &map_b, const MxPairArgs &p) const
     {
         if (lane == 0) {
-            dep_launch();
+            if (CODES) dep_launch();
             const MxGemmArgs &g = p.g;
+            const uint32_t leader_full = map_to_rank(full_bar(0), 0);
             int s = 0, used = 0;
             uint32_t ph = 1;
             bool live = true;
@@ -62,23 +69,24 @@ struct Mxf4Pair : MxCta {
                 int mt, nt;
                 pair_tile(p, t, mt, nt);
                 const int a_row = mt * kPairTile + rank * 128, b_row = nt * kPairTile + rank * 128;
-                const int a_tile = (mt * 2 + rank) * g.scale_tiles, b_tile = nt * 2 * g.scale_tiles;
                 for (int kb = 0; kb < g.k_blocks; ++kb) {
                     if (used >= kStages && !mbar_wait(empty_bar(s), ph, abort_flag, g.status, g.wait_limit)) { live = false; break; }
-                    const uint32_t at = smem + (uint32_t)(s * kRoom), bar = map_to_rank(full_bar(s), 0);
-                    if (rank == 0) mbar_expect_tx(full_bar(s), 2 * kBytes);
-                    tma_load_pair_2d(at, &map_a, bar, kb * kMxBK, a_row);
-                    tma_load_pair_2d(at + kHalf, &map_b, bar, kb * kMxBK, b_row);
-                    tma_load_pair_2d(at + kScalesAt, &map_sa, bar, 0, a_tile + kb * T);
-                    tma_load_pair_2d(at + kScalesAt + T * kScaleTile, &map_sb, bar, 0, b_tile + kb * T);
-                    tma_load_pair_2d(at + kScalesAt + 2 * T * kScaleTile, &map_sb, bar, 0, b_tile + g.scale_tiles + kb * T);
+                    const uint32_t at = smem + (uint32_t)(s * kRoom), bar = leader_full + 8u * (uint32_t)s;
+                    if (CODES) {
+                        if (rank == 0) mbar_expect_tx(full_bar(s), 2 * kBytes);
+                        tma_load_pair_2d(at, &map_a, bar, kb * kMxBK, a_row);
+                        tma_load_pair_2d(at + kHalf, &map_b, bar, kb * kMxBK, b_row);
+                    } else {
+                        tma_load_pair_3d(at + kScalesAt, &map_a, bar, 0, kb * T, mt * 2 + rank);
+                        tma_load_pair_3d(at + kScalesAt + T * kScaleTile, &map_b, bar, 0, kb * T, nt * 2);
+                    }
                     if (used < kStages) ++used;
                     if (++s == kStages) { s = 0; ph ^= 1u; }
                 }
             }
-            // After a wait that gave up no copy may land when the CTAs have left: the leader waits for what both announced, the
-            // other CTA for the leader at the cluster's barrier.
-            if (*abort_flag && rank == 0) {
+            // After a wait that gave up no copy may land when the CTAs have left: the leader waits for what was announced (in vain, up
+            // to the limit, where another producer stopped earlier), the other CTA for the leader at the cluster's barrier.
+            if (CODES && *abort_flag && rank == 0) {
                 for (int j = 0; j < used; ++j) {
                     const int q = s - 1 - j < 0 ? s - 1 - j + kStages : s - 1 - j;
                     // ph is flipped whenever the ring starts over: the parity of the last phase announced on stage q
@@ -131,70 +139,121 @@ struct Mxf4Pair : MxCta {
         __syncwarp();
     }
 
-    // 16 columns of a row.  WHOLE: all of them exist, outputs and bias on 32-byte boundaries.
-    template <bool WHOLE>
-    __device__ void put(const MxGemmArgs &g, const uint32_t *v, int64_t m, int64_t n, float alpha) const
+    // Scaling, bias and ReLU of C columns of a row.
+    template <int C>
+    __device__ void finish_row(const MxGemmArgs &g, float (&y)[C], int64_t n, float alpha) const
     {
-        if (m >= g.M || (!WHOLE && n >= g.N)) return;
-        const int cols = WHOLE || g.N - n >= 16 ? 16 : (int)(g.N - n);
-        float y[16];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) y[j] = __fmul_rn(__uint_as_float(v[j]), alpha);
+        for (int j = 0; j < C; ++j) y[j] = __fmul_rn(y[j], alpha);
         if (g.bias) {
-            float b[16];
-            load_run<false, WHOLE ? 32 : 0>(b, g.bias + n, cols);
+            if (n + C <= g.N && (reinterpret_cast<uintptr_t>(g.bias + n) & 15u) == 0) {
 #pragma unroll
-            for (int j = 0; j < 16; ++j) y[j] = __fadd_rn(y[j], b[j]);
+                for (int j = 0; j < C; j += 4) {
+                    const float4 b = __ldg(reinterpret_cast<const float4 *>(g.bias + n + j));
+                    y[j] = __fadd_rn(y[j], b.x);
+                    y[j + 1] = __fadd_rn(y[j + 1], b.y);
+                    y[j + 2] = __fadd_rn(y[j + 2], b.z);
+                    y[j + 3] = __fadd_rn(y[j + 3], b.w);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < C; ++j) y[j] = __fadd_rn(y[j], n + j < g.N ? __ldg(g.bias + n + j) : 0.0f);
+            }
         }
         if (g.relu) {
 #pragma unroll
-            for (int j = 0; j < 16; ++j) y[j] = y[j] > 0.0f ? y[j] : 0.0f;
+            for (int j = 0; j < C; ++j) y[j] = y[j] > 0.0f ? y[j] : 0.0f;
         }
-        const int64_t at = m * g.N + n;
-        if (g.f32_out) store_run<false, WHOLE ? 32 : 0>(g.f32_out + at, y, cols);
-        if (g.bf16_out) store_run<true, WHOLE ? 32 : 0>(g.bf16_out + at, y, cols);
     }
 
-    __device__ void finish(const MxPairArgs &p) const
+    // 32 rows x 128 bytes of one output through this warp's staging memory (rows of 128 bytes, swizzled as TMA does).
+    __device__ void store_box(const CUtensorMap &map, const uint32_t (&w)[32], uint32_t stage, int64_t m, int64_t n, const MxGemmArgs &g) const
+    {
+        if (lane == 0) tma_store_wait_read<0>();        // the box before has left
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" :: "r"(stage + (uint32_t)(lane * 128 + ((j ^ (lane & 7)) << 4))), "r"(w[4 * j]),
+                         "r"(w[4 * j + 1]), "r"(w[4 * j + 2]), "r"(w[4 * j + 3]) : "memory");
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0 && m < g.M && n < g.N) {
+            tma_store_2d(&map, stage, (int)n, (int)m);
+            tma_store_commit();
+        }
+    }
+
+    // 64 columns of 32 rows.  STAGED: rows of outputs start on 16-byte boundaries.
+    template <bool STAGED>
+    __device__ void put_span(const CUtensorMap &map_f, const CUtensorMap &map_h, const MxGemmArgs &g, const uint32_t (&v)[2][32], int64_t m0, int64_t n,
+                             float alpha) const
+    {
+        const uint32_t stage = smem + (uint32_t)(kStages * kRoom + (warp - 2) * kPairStaging);
+        uint32_t h[32];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            float y[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) y[j] = __uint_as_float(v[q][j]);
+            finish_row<32>(g, y, n + 32 * q, alpha);
+            if (STAGED) {
+                if (g.f32_out) {
+                    uint32_t f[32];
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) f[j] = __float_as_uint(y[j]);
+                    store_box(map_f, f, stage, m0, n + 32 * q, g);
+                }
+#pragma unroll
+                for (int j = 0; j < 16; ++j) h[16 * q + j] = bf16x2_of(y[2 * j], y[2 * j + 1]);
+            } else if (m0 + lane < g.M) {
+                // a row's pieces, element by element
+                const int64_t at = (m0 + lane) * g.N + n + 32 * q;
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    if (n + 32 * q + j >= g.N) continue;
+                    if (g.f32_out) g.f32_out[at + j] = y[j];
+                    if (g.bf16_out) g.bf16_out[at + j] = (uint16_t)bf16x2_of(y[j], 0.0f);
+                }
+            }
+        }
+        if (STAGED && g.bf16_out) store_box(map_h, h, stage, m0, n, g);
+    }
+
+    __device__ void finish(const CUtensorMap &map_f, const CUtensorMap &map_h, const MxPairArgs &p) const
     {
         const MxGemmArgs &g = p.g;
         const int quarter = warp & 3, half = (warp - 2) >> 2;
         const float alpha = mx_alpha(g);
-        const bool aligned = (g.N & (g.bf16_out ? 15 : 7)) == 0 &&
-                             ((reinterpret_cast<uintptr_t>(g.f32_out) | reinterpret_cast<uintptr_t>(g.bf16_out) | reinterpret_cast<uintptr_t>(g.bias)) & 31u) == 0;
         const uint32_t freed = map_to_rank(freed_bar(0), 0);
         int i = 0;
         for (int t = pair; t < tiles; t += p.pairs, ++i) {
             int mt, nt;
             pair_tile(p, t, mt, nt);
-            const int64_t m = (int64_t)mt * kPairTile + rank * 128 + quarter * 32 + lane, n0 = (int64_t)nt * kPairTile;
+            const int64_t m0 = (int64_t)mt * kPairTile + rank * 128 + quarter * 32, n0 = (int64_t)nt * kPairTile;
             mbar_wait(acc_bar(i & 1), (uint32_t)(i >> 1) & 1u, abort_flag, g.status, g.wait_limit);
             tc_fence_after();
             const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (i & 1) * kPairSecond;
-            const bool whole = aligned && n0 + kPairTile <= g.N;
-            // run r of 16 columns; the ones that the next tile's accumulator shares come first: 13, 14, 15 of the even tiles, 0, 1, 2 of the odd
-            auto run_of = [&](int q) { return (i & 1) ? q : q < 3 ? 13 + q : q - 3; };
+            // Spans of 64 columns, two for each half of the warps.  The one that holds the columns which the next tile's accumulator
+            // shares comes first: 3 of the even tiles, 0 of the odd ones.
+            const int first = (i & 1) ? 2 * half : 3 - 2 * half, second = (i & 1) ? first + 1 : first - 1;
 #pragma unroll 1
-            for (int q = half; q < 16; q += 4) {
-                const int ra = run_of(q), rb = run_of(q + 2);
-                uint32_t va[32], vb[32];
-                tmem_ld_32x16_issue(taddr + ra * 16, va);
-                tmem_ld_32x16_issue(taddr + rb * 16, vb);
+            for (int q = 0; q < 2; ++q) {
+                const int span = q ? second : first;
+                uint32_t v[2][32];
+                tmem_ld_32x32_issue(taddr + span * 64, v[0]);
+                tmem_ld_32x32_issue(taddr + span * 64 + 32, v[1]);
                 tmem_ld_wait();
-                if (q == half) {            // both of this warp's runs among the first three are in registers
+                if (q == 0) {
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive_remote(freed);
                 }
-                if (whole) {
-                    put<true>(g, va, m, n0 + ra * 16, alpha);
-                    put<true>(g, vb, m, n0 + rb * 16, alpha);
-                } else {
-                    put<false>(g, va, m, n0 + ra * 16, alpha);
-                    put<false>(g, vb, m, n0 + rb * 16, alpha);
-                }
+                if (p.staged) put_span<true>(map_f, map_h, g, v, m0, n0 + span * 64, alpha);
+                else put_span<false>(map_f, map_h, g, v, m0, n0 + span * 64, alpha);
             }
         }
+        if (lane == 0) tma_store_wait_all();
+        __syncwarp();
         tc_fence_before();
     }
 };
@@ -202,7 +261,8 @@ struct Mxf4Pair : MxCta {
 template <bool NV>
 __global__ void __launch_bounds__(kPairThreads)
 sparq_mxf4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_sa,
-                  const __grid_constant__ CUtensorMap map_sb, const MxPairArgs p)
+                  const __grid_constant__ CUtensorMap map_sb, const __grid_constant__ CUtensorMap map_f, const __grid_constant__ CUtensorMap map_h,
+                  const MxPairArgs p)
 {
     using Cta = Mxf4Pair<NV>;
     extern __shared__ uint8_t smem_raw[];
@@ -248,9 +308,10 @@ sparq_mxf4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     c.tmem = tmem_base_slot;
     dep_wait();
     switch (warp) {
-    case 0: c.produce(map_a, map_b, map_sa, map_sb, p); break;
+    case 0: c.template produce<true>(map_a, map_b, p); break;
     case 1: c.issue(p); break;
-    default: c.finish(p);
+    case kPairScaleWarp: c.template produce<false>(map_sa, map_sb, p); break;
+    default: c.finish(map_f, map_h, p);
     }
     // Neither CTA leaves, or gives its tensor memory back, while the pair's MMAs or the other's arrivals may reach it.
     tc_fence_before();
