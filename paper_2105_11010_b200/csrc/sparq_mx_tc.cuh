@@ -110,7 +110,7 @@ __device__ __forceinline__ void tc_commit_pair(uint32_t bar)
 }
 __device__ __forceinline__ void mbar_arrive_remote(uint32_t cluster_bar)
 {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(cluster_bar) : "memory");
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" :: "r"(cluster_bar) : "memory");
 }
 __device__ __forceinline__ void tc_copy_scales_pair(uint32_t taddr, uint64_t desc)
 {

@@ -26,11 +26,13 @@ struct WgradArgs {
 constexpr int kWgTokens = 64;                    // per reduction step: four MMAs of 16
 constexpr int kWgBox = kWgTokens * 128;          // 64 tokens x 64 bf16 columns
 
-// Scale 2^(code - 127 - 6) as a pair of equal bf16 values; NaN for the scale's NaN.
+// Scale 2^(code - 127 - 6) as a pair of equal bf16 values: an exponent of its own for codes 7 to 254, a subnormal below, NaN
+// for the scale's NaN.
 __device__ __forceinline__ uint32_t bf16_scale_pair(uint32_t code)
 {
-    const uint32_t b = code == kNanE8M0 ? 0x7FC0u : code > 6u ? (code - 6u) << 7 : 0x40u >> (6u - code);
-    return b * 0x00010001u;
+    uint32_t b = (code - 6u) << 7;
+    if (code - 7u > 247u) b = code == kNanE8M0 ? 0x7FC0u : 0x40u >> (6u - code);
+    return prmt(b, b, 0x1010u);
 }
 
 // Four codes of one block as bf16 values.  As bit patterns in bf16, whose steps are 1 in [128, 256) and 2 in [256, 512):
@@ -46,6 +48,27 @@ __device__ __forceinline__ void codes_to_bf16(uint32_t w, uint32_t scale, uint32
     };
     lo = two(prmt(w, 0u, 0x4140u));
     hi = two(prmt(w, 0u, 0x4342u));
+}
+
+// ITEMS times eight codes of a thread -- of tokens `STEP` apart, in a raw tile with rows of 128 codes and of 16 scales -- into an
+// operand tile.  All loads go out before the first store: one item after the other took a stage 1.2 us, chains of latency.
+template <int ITEMS, int STEP>
+__device__ __forceinline__ void transform_codes(uint32_t src, uint32_t sc, uint32_t dst)
+{
+    uint32_t a[ITEMS], b[ITEMS], code[ITEMS];
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j) {
+        asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(a[j]), "=r"(b[j]) : "r"(src + (uint32_t)(j * STEP * 128)));
+        asm volatile("ld.shared.u8 %0, [%1];" : "=r"(code[j]) : "r"(sc + (uint32_t)(j * STEP * 16)));
+    }
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j) {
+        const uint32_t scale = bf16_scale_pair(code[j]);
+        uint32_t x0, x1, x2, x3;
+        codes_to_bf16(a[j], scale, x0, x1);
+        codes_to_bf16(b[j], scale, x2, x3);
+        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" :: "r"(dst + (uint32_t)(j * STEP * 128)), "r"(x0), "r"(x1), "r"(x2), "r"(x3) : "memory");
+    }
 }
 
 // The tensor cores cut a running sum off where fp32 would round it, so its error grows with the number of additions and
@@ -163,16 +186,7 @@ struct WgradSmall : MxCta {
         for (int it = 0; it < steps; ++it) {
             mbar_wait(full_bar(s), ph, abort_flag, g.status, g.wait_limit);
             const uint32_t at = smem + (uint32_t)(s * kWgStage);
-#pragma unroll
-            for (int j = 0; j < kWgTokens / 16; ++j) {
-                uint32_t a, b, code, x0, x1, x2, x3;
-                asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(a), "=r"(b) : "r"(at + src + (uint32_t)(j * 16 * kWgBN)));
-                asm volatile("ld.shared.u8 %0, [%1];" : "=r"(code) : "r"(at + sc + (uint32_t)(j * 16 * 16)));
-                const uint32_t scale = bf16_scale_pair(code);
-                codes_to_bf16(a, scale, x0, x1);
-                codes_to_bf16(b, scale, x2, x3);
-                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" :: "r"(at + dst + (uint32_t)(j * 16 * 128)), "r"(x0), "r"(x1), "r"(x2), "r"(x3) : "memory");
-            }
+            transform_codes<kWgTokens / 16, 16>(at + src, at + sc, at + dst);
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(xf_bar(s));
@@ -315,6 +329,293 @@ sparq_wgrad_small_kernel(const __grid_constant__ CUtensorMap map_dy, const __gri
     if (warp == 1) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(c.tmem), "r"(2u * kWgBN) : "memory");
+    }
+}
+
+// ---- many output tiles -----------------------------------------------------------------------------------
+// A persistent pair of CTAs walks tiles of 256 x 256: one MMA (cta_group::2) multiplies 256 columns of dy by 256 of X.  Each CTA
+// brings its 128 columns of dy, and brings and transforms its 128 columns of X: a value of X is transformed once per row of tiles
+// of 256, half as often as with one CTA by itself, and neither the transform (8192 values a step and SM, about 200 of
+// its 512 cycles of issue) nor shared memory (81 KB a step, of 64 KB the MMAs alone) holds the tensor cores up much.
+// X16: X comes as bf16 (the library's own, expanded from the codes by the launch before) and goes from TMA to the MMA; the workers
+// only add up.  Same operands, same order of sums, same bits.
+// Warps: 0 producer of dy, 2 of codes and scales, 1 tensor memory and (leader) MMA issue, 4..11 workers, each thread with 128
+// columns of a row in registers.
+
+constexpr int kWgTile = 256;
+constexpr int kWgPairOwn = 128;                  // columns of a worker thread's row
+constexpr int kWgCodeWarp = 2;
+constexpr int kWgFirstWorker = 4;                // whole groups of four warps, for setmaxnreg
+constexpr int kWgPairThreads = 32 * (kWgFirstWorker + kWgWorkers);
+
+constexpr int kWgStages16 = 7;
+__host__ __device__ constexpr int wgrad_smem(bool x16) { return 1024 + (x16 ? kWgStages16 * 4 * kWgBox : kWgStages * kWgStage); }
+
+struct WgradPairArgs {
+    WgradArgs g;
+    int n_tiles, k_tiles, pairs;
+};
+
+// Tile t in an order that keeps eight rows of tiles together.
+__device__ __forceinline__ void wgrad_tile(const WgradPairArgs &p, int t, int &nt, int &kt)
+{
+    const int per_group = 8 * p.k_tiles, group = t / per_group, first = group * 8;
+    const int rows = p.n_tiles - first < 8 ? p.n_tiles - first : 8, in = t - group * per_group;
+    kt = in / rows;
+    nt = first + in - kt * rows;
+}
+
+// full: dy of both CTAs, in the leader; raw: codes and scales of this CTA; xf: transformed by both CTAs' workers,
+// in the leader; empty: the MMAs that read the stage have retired; acc, freed: as above.
+template <bool X16>
+struct WgradPair : MxCta {
+    static constexpr int kXAt = X16 ? 2 * kWgBox : kWgX, kStage = kXAt + 2 * kWgBox, kStages = X16 ? kWgStages16 : kWgStages;
+    int tiles, pair;
+    __device__ uint32_t raw_bar(int s) const { return bars + (uint32_t)sizeof(MxBars) + (uint32_t)s * 8u; }
+
+    template <bool DY>
+    __device__ void produce(const CUtensorMap &map_a, const CUtensorMap &map_b, const WgradPairArgs &p) const
+    {
+        if (lane == 0) {
+            if (DY) dep_launch();
+            const WgradArgs &g = p.g;
+            const uint32_t leader_full = map_to_rank(full_bar(0), 0);
+            int s = 0, used = 0;
+            uint32_t ph = 1;
+            bool live = true;
+            for (int t = pair; t < tiles && live; t += p.pairs) {
+                int nt, kt;
+                wgrad_tile(p, t, nt, kt);
+                const int n = nt * kWgTile + rank * 128, k = kt * kWgTile + rank * 128, sc = (k / 32) & ~15;
+                for (int b = 0; b < g.blocks; ++b) {
+                    if (used >= kStages && !mbar_wait(empty_bar(s), ph, abort_flag, g.status, g.wait_limit)) { live = false; break; }
+                    const uint32_t at = smem + (uint32_t)(s * kStage);
+                    const int m = b * kWgTokens;
+                    if (DY) {
+                        const uint32_t bar = leader_full + 8u * (uint32_t)s;
+                        if (rank == 0) mbar_expect_tx(full_bar(s), (X16 ? 8 : 4) * kWgBox);
+                        tma_load_pair_2d(at, &map_a, bar, n, m);
+                        tma_load_pair_2d(at + kWgBox, &map_a, bar, n + 64, m);
+                    } else if (X16) {
+                        const uint32_t bar = leader_full + 8u * (uint32_t)s;
+                        tma_load_pair_2d(at + kXAt, &map_a, bar, k, m);
+                        tma_load_pair_2d(at + kXAt + kWgBox, &map_a, bar, k + 64, m);
+                    } else {
+                        mbar_expect_tx(raw_bar(s), kWgX - kWgCodes);
+                        tma_load_2d(at + kWgCodes, &map_a, raw_bar(s), k, m);
+                        tma_load_2d(at + kWgScales, &map_b, raw_bar(s), sc, m);
+                    }
+                    if (used < kStages) ++used;
+                    if (++s == kStages) { s = 0; ph ^= 1u; }
+                }
+            }
+            // After a wait that gave up no copy may land when the CTAs have left: each waits for the codes that it announced, the leader for
+            // both CTAs' dy (in vain, up to the limit, where the other producer stopped earlier), the other CTA for the leader at the
+            // cluster's barrier.
+            if (*abort_flag && (DY ? rank == 0 : !X16)) {
+                for (int j = 0; j < used; ++j) {
+                    const int q = s - 1 - j < 0 ? s - 1 - j + kStages : s - 1 - j;
+                    // ph is flipped whenever the ring starts over: the parity of the last phase announced on stage q
+                    mbar_wait(DY ? full_bar(q) : raw_bar(q), q < s ? ph ^ 1u : ph, abort_flag, g.status, g.wait_limit, true);
+                }
+            }
+        }
+        __syncwarp();
+    }
+
+    // Chunks are counted through all tiles: chunk c adds up in accumulator c & 1.
+    __device__ void issue(const WgradPairArgs &p) const
+    {
+        if (rank == 0) {
+            const WgradArgs &g = p.g;
+            const uint32_t elected = elect_one();
+            constexpr uint32_t id = make_idesc_bf16_mn(kWgTile, 256);
+            int s = 0, c = 0;
+            uint32_t ph = 0;
+            for (int t = pair; t < tiles; t += p.pairs) {
+                for (int b = 0; b < g.blocks; ++b) {
+                    const int in = b & (kWgChunkSteps - 1);
+                    if (in == 0 && c >= 2) mbar_wait(freed_bar(c & 1), (uint32_t)((c >> 1) - 1) & 1u, abort_flag, g.status, g.wait_limit);
+                    mbar_wait(full_bar(s), ph, abort_flag, g.status, g.wait_limit);
+                    if (!X16) mbar_wait(xf_bar(s), ph, abort_flag, g.status, g.wait_limit);
+                    tc_fence_after();
+                    const bool chunk_ends = in == kWgChunkSteps - 1 || b == g.blocks - 1;
+                    if (elected) {
+                        const uint32_t at = smem + (uint32_t)(s * kStage), d = tmem + (uint32_t)((c & 1) * kWgTile);
+                        const uint64_t adesc = mn_major_desc(at, kWgBox), bdesc = mn_major_desc(at + kXAt, kWgBox);
+#pragma unroll
+                        for (int k = 0; k < kWgTokens / 16; ++k)
+                            tc_mma_bf16_pair(d, adesc + (uint64_t)(k * 128), bdesc + (uint64_t)(k * 128), id, (in > 0 || k > 0) ? 1u : 0u);
+                        tc_commit_pair(empty_bar(s));
+                        if (chunk_ends) tc_commit_pair(acc_bar(c & 1));
+                    }
+                    __syncwarp();
+                    if (chunk_ends) ++c;
+                    if (++s == kStages) { s = 0; ph ^= 1u; }
+                }
+            }
+            // every MMA has retired before the warp goes on
+            if (c > 0) mbar_wait(acc_bar((c - 1) & 1), (uint32_t)((c - 1) >> 1) & 1u, abort_flag, g.status, g.wait_limit, true);
+        }
+        __syncwarp();
+    }
+
+    __device__ void add_chunk(const WgradArgs &g, int c, uint32_t leader_freed, float (&sum)[kWgPairOwn]) const
+    {
+        mbar_wait(acc_bar(c & 1), (uint32_t)(c >> 1) & 1u, abort_flag, g.status, g.wait_limit);
+        tc_fence_after();
+        const uint32_t taddr = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)((c & 1) * kWgTile + ((warp - kWgFirstWorker) >> 2) * kWgPairOwn);
+#pragma unroll
+        for (int h = 0; h < kWgPairOwn / 16; ++h) {
+            uint32_t v[32];
+            tmem_ld_32x16_issue(taddr + h * 16, v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 16; ++j) sum[h * 16 + j] = __fadd_rn(sum[h * 16 + j], __uint_as_float(v[j]));
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_remote(leader_freed + 8u * (uint32_t)(c & 1));
+    }
+
+    __device__ void write(const WgradArgs &g, int64_t n, int64_t k, const float (&sum)[kWgPairOwn]) const
+    {
+        if (n >= g.N) return;
+        float *out = g.dw + n * g.K + k;
+        if (k + kWgPairOwn <= g.K && (reinterpret_cast<uintptr_t>(out) & 31u) == 0) {
+#pragma unroll
+            for (int j = 0; j < kWgPairOwn; j += 8) {
+                uint32_t v[8];
+                if (g.accumulate) {
+                    ld_v8(v, out + j);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = __float_as_uint(__fadd_rn(__uint_as_float(v[i]), sum[j + i]));
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = __float_as_uint(sum[j + i]);
+                }
+                st_v8(out + j, v);
+            }
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < kWgPairOwn; ++j)
+            if (k + j < g.K) out[j] = g.accumulate ? __fadd_rn(out[j], sum[j]) : sum[j];
+    }
+
+    __device__ void work(const WgradPairArgs &p) const
+    {
+        const WgradArgs &g = p.g;
+        // a team of four warps takes every other stage: one's barriers and loads run beside the other's arithmetic
+        const int team = (warp - kWgFirstWorker) >> 2, wt = threadIdx.x & 127, chunk = wt & 15, t0 = wt >> 4;    // eight codes of every eighth token
+        const uint32_t src = kWgCodes + (uint32_t)(t0 * kWgBN + chunk * 8);
+        const uint32_t dst = kWgX + (uint32_t)((chunk >> 3) * kWgBox + t0 * 128 + (((chunk & 7) ^ t0) << 4));
+        const uint32_t leader_xf = map_to_rank(xf_bar(0), 0), leader_freed = map_to_rank(freed_bar(0), 0);
+        int s = 0, c = 0, stage = 0;
+        uint32_t ph = 0;
+        for (int t = pair; t < tiles; t += p.pairs) {
+            int nt, kt;
+            wgrad_tile(p, t, nt, kt);
+            const int k0 = kt * kWgTile + rank * 128;
+            const uint32_t sc = kWgScales + (uint32_t)(t0 * 16 + ((k0 / 32) & 15) + (chunk >> 2));
+            float sum[kWgPairOwn];
+#pragma unroll
+            for (int j = 0; j < kWgPairOwn; ++j) sum[j] = 0.0f;
+            const int c_first = c;
+            for (int b = 0; b < g.blocks; ++b) {
+                if (!X16 && (stage++ & 1) == team) {
+                    mbar_wait(raw_bar(s), ph, abort_flag, g.status, g.wait_limit);
+                    const uint32_t at = smem + (uint32_t)(s * kStage);
+                    transform_codes<kWgTokens / 8, 8>(at + src, at + sc, at + dst);
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_remote(leader_xf + 8u * (uint32_t)s);
+                }
+                if (!X16 && ++s == kStages) { s = 0; ph ^= 1u; }
+                if ((b & (kWgChunkSteps - 1)) == kWgChunkSteps - 1 && b < g.blocks - 1) {
+                    if (c > c_first) add_chunk(g, c - 1, leader_freed, sum);
+                    ++c;
+                }
+            }
+            if (c > c_first) add_chunk(g, c - 1, leader_freed, sum);
+            add_chunk(g, c, leader_freed, sum);
+            ++c;
+            write(g, (int64_t)nt * kWgTile + rank * 128 + (warp & 3) * 32 + lane, (int64_t)kt * kWgTile + ((warp - kWgFirstWorker) >> 2) * kWgPairOwn, sum);
+        }
+    }
+};
+
+template <bool X16>
+__global__ void __launch_bounds__(kWgPairThreads, 1)
+sparq_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUtensorMap map_codes,
+                   const __grid_constant__ CUtensorMap map_scales, const WgradPairArgs p)
+{
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) struct { MxBars bars; uint64_t raw[kMaxStages]; } room;
+    __shared__ uint32_t tmem_base_slot;
+    __shared__ uint32_t abort_word;
+
+    using Cta = WgradPair<X16>;
+    Cta c;
+    const int warp = c.warp = threadIdx.x >> 5, lane = c.lane = threadIdx.x & 31;
+    c.abort_flag = &abort_word;
+    c.smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    c.bars = smem_u32(&room);
+    c.rank = (int)(blockIdx.x & 1u);
+    c.pair = (int)(blockIdx.x >> 1);
+    c.tiles = p.n_tiles * p.k_tiles;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            prefetch_tensormap(&map_dy);
+            prefetch_tensormap(&map_codes);
+            prefetch_tensormap(&map_scales);
+            for (int s = 0; s < Cta::kStages; ++s) {
+                mbar_init(c.full_bar(s), 1);
+                mbar_init(c.raw_bar(s), 1);
+                mbar_init(c.xf_bar(s), 2 * 4);         // a team of each CTA
+                mbar_init(c.empty_bar(s), 1);
+            }
+            for (int b = 0; b < 2; ++b) {
+                mbar_init(c.acc_bar(b), 1);
+                mbar_init(c.freed_bar(b), 2 * kWgWorkers);
+            }
+            abort_word = 0;
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(smem_u32(&tmem_base_slot)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_arrive();          // both CTAs have their barriers and their tensor memory
+    cluster_wait();
+    tc_fence_after();
+    c.tmem = tmem_base_slot;
+    dep_wait();
+    // Registers: 384 threads were launched with 168 each; of the same 64512, the workers take 216 and the first four warps 72.
+    if (warp >= kWgFirstWorker) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        c.work(p);
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        switch (warp) {
+        case 0: c.template produce<true>(map_dy, map_dy, p); break;
+        case 1: c.issue(p); break;
+        case kWgCodeWarp: c.template produce<false>(map_codes, map_scales, p); break;
+        default: break;
+        }
+    }
+    // Neither CTA leaves, or gives its tensor memory back, while the pair's MMAs or the other's arrivals may reach it.
+    tc_fence_before();
+    __syncthreads();
+    cluster_arrive();
+    cluster_wait();
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" :: "r"(c.tmem), "r"(512u) : "memory");
     }
 }
 
