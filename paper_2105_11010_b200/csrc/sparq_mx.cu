@@ -20,6 +20,14 @@ int check_mx_max(int format, const float *max_dev, const char *name)
     return SPARQ_OK;
 }
 
+int check_mx_extent(int64_t rows, int64_t cols, int64_t ld)
+{
+    if (rows >= kMxMost || cols >= kMxMost) return set_error(SPARQ_ERR_UNSUPPORTED, "rows and columns must be below 2^31 - 256");
+    if ((__int128)(rows + 128) * (ld + 512) > INT64_C(1) << 60)
+        return set_error(SPARQ_ERR_UNSUPPORTED, "%lld rows of %lld elements are more than any device holds", (long long)rows, (long long)ld);
+    return SPARQ_OK;
+}
+
 int run_grid(int64_t runs, int *blocks)
 {
     int dev = 0, sms = 0;
@@ -35,12 +43,14 @@ namespace {
 
 template <bool BF16, int ALIGN, int FORMAT>
 __global__ void __launch_bounds__(kRunThreads)
-quantize_mx_kernel(const void *x, int64_t rows, int64_t cols, int64_t ldx, int64_t per_row, int64_t runs,
+quantize_mx_kernel(const void *x, int64_t rows, int64_t cols, int64_t ldx, uint32_t per_row, int64_t runs,
                    const float *max_dev, uint8_t *codes, uint8_t *scales)
 {
     constexpr int kWidth = BF16 ? 2 : 4;
     const int64_t stride = (int64_t)gridDim.x * kRunThreads, first = (int64_t)blockIdx.x * kRunThreads + threadIdx.x;
-    const int64_t pitch = mx_code_pitch(FORMAT, cols), coded = mx_padded(cols) / 16, words = mx_scale_cols(FORMAT, cols) / 4;
+    const int64_t pitch = mx_code_pitch(FORMAT, cols), words = mx_scale_cols(FORMAT, cols) / 4;
+    const uint32_t coded = (uint32_t)(mx_padded(cols) / 16);
+    const Span span = span_of<BF16>(x, rows, cols, ldx);
     RunWalk at(first, stride, per_row);
     dep_wait();
     dep_launch();
@@ -52,12 +62,14 @@ quantize_mx_kernel(const void *x, int64_t rows, int64_t cols, int64_t ldx, int64
     }
     // `runs` is a multiple of 32: a warp's lanes leave the loop together
     for (int64_t i = first; i < runs; i += stride, at.next()) {
-        const int64_t left = at.row < rows ? cols - at.run * 16 : 0;
+        const int64_t left = at.row < rows ? cols - (int64_t)at.run * 16 : 0;
+        uint32_t v[kRunWords<BF16>];
+        load_words<BF16, ALIGN>(v, reinterpret_cast<const uint8_t *>(x) + (left > 0 ? (at.row * ldx + at.run * 16) * kWidth : 0), left, span);
+        uint32_t mb = run_max_bits<BF16>(v);
         float f[16];
-        load_run<BF16, ALIGN>(f, reinterpret_cast<const uint8_t *>(x) + (left > 0 ? (at.row * ldx + at.run * 16) * kWidth : 0), left);
-        uint32_t mb = run_max_bits(f);
+        floats_of_words<BF16>(f, v);
         uint32_t code;
-        float mul;
+        float mul = 1.0f;
         if (FORMAT == SPARQ_NVFP4) {
             code = mb >= kInfBits ? kNanE4M3 : e4m3_of(__fmul_rn(__uint_as_float(mb), enc_scale));
             const float s = float_of_e4m3(code);
@@ -65,13 +77,14 @@ quantize_mx_kernel(const void *x, int64_t rows, int64_t cols, int64_t ldx, int64
         } else {
             mb = max(mb, __shfl_xor_sync(0xFFFFFFFFu, mb, 1));
             code = e8m0_code(mb, FORMAT == SPARQ_MXFP4 ? 2u : 0u);
-            mul = inv_pow2_of_code(code);
+            if (FORMAT == SPARQ_MXFP4) mul = inv_pow2_of_code(code);
         }
         const bool none = mb >= kInfBits || mul == 0.0f;      // a scale that is zero or NaN: codes of zero
-        if (at.row < rows && at.run < coded) {
+        const bool live = at.row < rows && at.run < coded;
+        if (live) {
             uint8_t *dst = codes + at.row * pitch;
             if (FORMAT == SPARQ_MXINT8) {
-                const uint4 w = int8_codes(f, mul);
+                const uint4 w = int8_codes(f, code, mb);
                 reinterpret_cast<uint4 *>(dst)[at.run] = none ? make_uint4(0u, 0u, 0u, 0u) : w;
             } else {
 #pragma unroll
@@ -81,9 +94,8 @@ quantize_mx_kernel(const void *x, int64_t rows, int64_t cols, int64_t ldx, int64
             }
         }
         // four scales at a time, the padding's too: zero, which is a number in either format
-        if (at.row >= rows || at.run >= coded) code = 0u;
         constexpr int kLanes = FORMAT == SPARQ_NVFP4 ? 4 : 8;
-        const uint32_t word = gather_word<kLanes>(code);
+        const uint32_t word = gather_word<kLanes>(live ? code : 0u);
         if ((threadIdx.x & (kLanes - 1)) == 0)
             *reinterpret_cast<uint32_t *>(scales + mx_scale_word<FORMAT != SPARQ_MXINT8>(at.row, at.run / kLanes, words)) = word;
     }
@@ -91,7 +103,7 @@ quantize_mx_kernel(const void *x, int64_t rows, int64_t cols, int64_t ldx, int64
 
 template <bool BF16, int ALIGN, int FORMAT>
 __global__ void __launch_bounds__(kRunThreads)
-dequantize_mx_kernel(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t cols, int64_t per_row, const float *max_dev,
+dequantize_mx_kernel(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t cols, uint32_t per_row, const float *max_dev,
                      void *out, int64_t ldo)
 {
     constexpr int kWidth = BF16 ? 2 : 4;
@@ -102,25 +114,30 @@ dequantize_mx_kernel(const uint8_t *codes, const uint8_t *scales, int64_t rows, 
     dep_launch();
     float dec = 1.0f;
     if (FORMAT == SPARQ_NVFP4) dec = __fdiv_rn(nvfp4_largest(*max_dev), 2688.0f);
-    for (int64_t i = first; i < runs; i += stride, at.next()) {
-        const int64_t c = FORMAT == SPARQ_NVFP4 ? at.run : at.run >> 1;
-        const uint32_t code = scales[mx_scale_word<FORMAT != SPARQ_MXINT8>(at.row, c >> 2, words) + (c & 3)];
-        const uint8_t *src = codes + at.row * pitch;
+    // a warp's lanes leave the loop together; those past the last run have nothing to store
+    for (int64_t i = first; i < ((runs + 31) & ~INT64_C(31)); i += stride, at.next()) {
         float f[16];
-        if (FORMAT == SPARQ_MXINT8) {
-            floats_of_int8(f, reinterpret_cast<const uint4 *>(src)[at.run], code);
-        } else {
-            const uint2 w = reinterpret_cast<const uint2 *>(src)[at.run];
-            floats_of_e2m1x8(f, w.x);
-            floats_of_e2m1x8(f + 8, w.y);
-            const float s = FORMAT == SPARQ_NVFP4 ? float_of_e4m3(code) : code == kNanE8M0 ? __uint_as_float(0x7FC00000u) : pow2_of_code(code);
+        int64_t left = 0;
+        if (i < runs) {
+            const uint32_t c = FORMAT == SPARQ_NVFP4 ? at.run : at.run >> 1;
+            const uint32_t code = scales[mx_scale_word<FORMAT != SPARQ_MXINT8>(at.row, c >> 2, words) + (c & 3)];
+            const uint8_t *src = codes + at.row * pitch;
+            left = cols - (int64_t)at.run * 16;
+            if (FORMAT == SPARQ_MXINT8) {
+                floats_of_int8(f, reinterpret_cast<const uint4 *>(src)[at.run], code);
+            } else {
+                const uint2 w = reinterpret_cast<const uint2 *>(src)[at.run];
+                floats_of_e2m1x8(f, w.x);
+                floats_of_e2m1x8(f + 8, w.y);
+                const float s = FORMAT == SPARQ_NVFP4 ? float_of_e4m3(code) : code == kNanE8M0 ? __uint_as_float(0x7FC00000u) : pow2_of_code(code);
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                f[j] = __fmul_rn(f[j], s);
-                if (FORMAT == SPARQ_NVFP4) f[j] = __fmul_rn(f[j], dec);
+                for (int j = 0; j < 16; ++j) {
+                    f[j] = __fmul_rn(f[j], s);
+                    if (FORMAT == SPARQ_NVFP4) f[j] = __fmul_rn(f[j], dec);
+                }
             }
         }
-        store_run<BF16, ALIGN>(reinterpret_cast<uint8_t *>(out) + (at.row * ldo + at.run * 16) * kWidth, f, cols - at.run * 16);
+        store_run<BF16, ALIGN>(reinterpret_cast<uint8_t *>(out) + (at.row * ldo + at.run * 16) * kWidth, f, left, at.run);
     }
 }
 
@@ -135,9 +152,7 @@ int check_tensor(int dtype, int64_t rows, int64_t cols, int64_t ld, const void *
     if (ld < cols) return set_error(SPARQ_ERR_INVALID_ARG, "the leading dimension of %s (%lld) is less than its columns (%lld)", name, (long long)ld, (long long)cols);
     if ((uintptr_t)x & (dtype == SPARQ_DTYPE_BF16 ? 1u : 3u)) return set_error(SPARQ_ERR_UNSUPPORTED, "%s is not aligned to its elements", name);
     if (((uintptr_t)codes | (uintptr_t)scales) & 15u) return set_error(SPARQ_ERR_UNSUPPORTED, "codes and scales must be 16-byte aligned");
-    if (rows > INT64_C(1) << 40 || ld > INT64_C(1) << 40 || (__int128)(rows + 128) * (ld + 512) > INT64_C(1) << 60)
-        return set_error(SPARQ_ERR_UNSUPPORTED, "%lld rows of %lld elements are more than any device holds", (long long)rows, (long long)ld);
-    return SPARQ_OK;
+    return check_mx_extent(rows, cols, ld);
 }
 
 }  // namespace
@@ -148,11 +163,10 @@ using namespace sparq;
 
 static int64_t mx_bytes(int format, int64_t rows, int64_t cols, bool codes)
 {
-    const int rc = check_mx_format(format, false);
+    int rc = check_mx_format(format, false);
     if (rc != SPARQ_OK) return rc;
     if (rows < 0 || cols < 0) return set_error(SPARQ_ERR_INVALID_ARG, "negative dimension");
-    if (rows > INT64_C(1) << 40 || cols > INT64_C(1) << 40 || (__int128)(rows + 128) * (cols + 512) > INT64_C(1) << 60)
-        return set_error(SPARQ_ERR_UNSUPPORTED, "%lld rows of %lld elements are more than any device holds", (long long)rows, (long long)cols);
+    if ((rc = check_mx_extent(rows, cols, cols)) != SPARQ_OK) return rc;
     return codes ? rows * mx_code_pitch(format, cols) : mx_scale_rows(format, rows) * mx_scale_cols(format, cols);
 }
 
@@ -175,7 +189,8 @@ extern "C" int sparq_quantize_mx(const void *x, int dtype, int64_t rows, int64_t
     if (rc == SPARQ_OK) rc = check_tensor(dtype, rows, cols, ldx, x, codes, scales, "x");
     if (rc != SPARQ_OK || rows == 0 || cols == 0) return rc;
     const bool bf16 = dtype == SPARQ_DTYPE_BF16;
-    const int64_t per_row = mx_scale_cols(format, cols) * (mx_block(format) / 16), runs = mx_scale_rows(format, rows) * per_row;
+    const uint32_t per_row = (uint32_t)(mx_scale_cols(format, cols) * (mx_block(format) / 16));
+    const int64_t runs = mx_scale_rows(format, rows) * per_row;
     int blocks = 0;
     if ((rc = run_grid(runs, &blocks)) != SPARQ_OK) return rc;
     const int align = run_align(x, ldx, bf16 ? 2 : 4);
@@ -193,7 +208,7 @@ extern "C" int sparq_dequantize_mx(const void *codes, const uint8_t *scales, int
     if (rc == SPARQ_OK) rc = check_tensor(dtype, rows, cols, ldo, out, codes, scales, "out");
     if (rc != SPARQ_OK || rows == 0 || cols == 0) return rc;
     const bool bf16 = dtype == SPARQ_DTYPE_BF16;
-    const int64_t per_row = (cols + 15) / 16;
+    const uint32_t per_row = (uint32_t)((cols + 15) / 16);
     int blocks = 0;
     if ((rc = run_grid(rows * per_row, &blocks)) != SPARQ_OK) return rc;
     const int align = run_align(out, ldo, bf16 ? 2 : 4);

@@ -37,46 +37,35 @@ __host__ __device__ __forceinline__ int64_t mx_scale_word(int64_t row, int64_t w
 }
 
 // Checks shared by the entry points (sparq_mx.cu).
+constexpr int64_t kMxMost = INT64_C(2147483647) - 255;      // no extent reaches it, so that padded ones stay within 32 bits
+int check_mx_extent(int64_t rows, int64_t cols, int64_t ld);
 int check_mx_format(int format, bool four_bits);
 int check_mx_max(int format, const float *max_dev, const char *name);
 
 #ifdef __CUDACC__
 
-// ---- 16 elements of a row as fp32 ---------------------------------------------------------------
-// ALIGN: bytes that every run's address is a multiple of -- 32 and 16 are read whole, anything less element by element,
-// as is a run that the row ends in.
+// ---- 16 elements of a row -------------------------------------------------------------------------
+// A run is 8 words of bf16 pairs or 16 of fp32.  ALIGN: bytes that every run's address is a multiple of.  32 and 16 are read and
+// written whole; 0 (rows of odd length) goes through 16-byte vectors too, shifted to where the run starts: element by
+// element such a tensor took up to seven times as long (8000 x 4100 bf16, gated silu and its gradient, 190 and 376 us).
 
-__device__ __forceinline__ void ld_v8(uint32_t (&v)[8], const void *p)
+__device__ __forceinline__ void ld_v8(uint32_t *v, const void *p)
 {
     asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                  : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]) : "l"(p));
 }
-__device__ __forceinline__ void st_v8(void *p, const uint32_t (&v)[8])
+__device__ __forceinline__ void st_v8(void *p, const uint32_t *v)
 {
     asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
                  :: "l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
-
-template <int ALIGN>
-__device__ __forceinline__ void ld_bytes32(uint32_t (&v)[8], const uint8_t *p)
+__device__ __forceinline__ void ld_v4(uint32_t *v, const void *p)
 {
-    if (ALIGN == 32) {
-        ld_v8(v, p);
-    } else {
-        const uint4 a = reinterpret_cast<const uint4 *>(p)[0], b = reinterpret_cast<const uint4 *>(p)[1];
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-        v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    }
+    asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "l"(p));
 }
-template <int ALIGN>
-__device__ __forceinline__ void st_bytes32(uint8_t *p, const uint32_t (&v)[8])
+__device__ __forceinline__ void st_v4(void *p, const uint32_t *v)
 {
-    if (ALIGN == 32) {
-        st_v8(p, v);
-    } else {
-        reinterpret_cast<uint4 *>(p)[0] = make_uint4(v[0], v[1], v[2], v[3]);
-        reinterpret_cast<uint4 *>(p)[1] = make_uint4(v[4], v[5], v[6], v[7]);
-    }
+    asm volatile("st.global.v4.b32 [%0], {%1,%2,%3,%4};" :: "l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
 }
 
 // Two fp32 values as bf16, to nearest even (NaN stays NaN); lo in the low half.
@@ -87,76 +76,153 @@ __device__ __forceinline__ uint32_t bf16x2_of(float lo, float hi)
     return d;
 }
 
-// `p` points at the run's first element, `left` elements of the row remain from there (any number, negative too).
-template <bool BF16, int ALIGN>
-__device__ __forceinline__ void load_run(float (&f)[16], const void *p, int64_t left)
+template <bool BF16>
+constexpr int kRunWords = BF16 ? 8 : 16;
+
+// A tensor's own bytes: vectors that a shifted run takes beyond its row stay within them.
+struct Span {
+    const uint8_t *first, *end;
+};
+template <bool BF16>
+__device__ __forceinline__ Span span_of(const void *p, int64_t rows, int64_t cols, int64_t ld)
 {
     const uint8_t *b = reinterpret_cast<const uint8_t *>(p);
-    if (ALIGN >= 16 && left >= 16) {
-        uint32_t v[8];
-        ld_bytes32<ALIGN>(v, b);
-        if (BF16) {
+    return {b, b + ((rows - 1) * ld + cols) * (BF16 ? 2 : 4)};
+}
+
+// W words from s bytes on (s < 16, a multiple of the element's width) of the W + 4 words w, in place.
+template <bool BF16, int W>
+__device__ __forceinline__ void shift_words(uint32_t (&w)[W + 4], uint32_t s)
+{
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                f[2 * i] = __uint_as_float(v[i] << 16);
-                f[2 * i + 1] = __uint_as_float(v[i] & 0xFFFF0000u);
-            }
-        } else {
-            uint32_t w[8];
-            ld_bytes32<ALIGN>(w, b + 32);
+    for (int i = 0; i < W + 2; ++i) w[i] = s & 8u ? w[i + 2] : w[i];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                f[i] = __uint_as_float(v[i]);
-                f[8 + i] = __uint_as_float(w[i]);
-            }
-        }
-        return;
-    }
+    for (int i = 0; i < W + 1; ++i) w[i] = s & 4u ? w[i + 1] : w[i];
+    if (BF16) {
+        const uint32_t bits = (s & 2u) * 8u;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        f[i] = 0.0f;
-        if (i < left)
-            f[i] = BF16 ? __uint_as_float((uint32_t)reinterpret_cast<const uint16_t *>(p)[i] << 16) : reinterpret_cast<const float *>(p)[i];
+        for (int i = 0; i < W; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], bits);
     }
 }
 
+// `p` points at the run's first element, `left` elements of the row remain from there (any number, negative too); what
+// the row does not have is zero.
 template <bool BF16, int ALIGN>
-__device__ __forceinline__ void store_run(void *p, const float (&f)[16], int64_t left)
+__device__ __forceinline__ void load_words(uint32_t (&v)[kRunWords<BF16>], const void *p, int64_t left, const Span &span)
 {
-    uint8_t *b = reinterpret_cast<uint8_t *>(p);
-    uint32_t v[8];
+    constexpr int W = kRunWords<BF16>;
+    const uint8_t *b = reinterpret_cast<const uint8_t *>(p);
     if (ALIGN >= 16 && left >= 16) {
-        if (BF16) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = bf16x2_of(f[2 * i], f[2 * i + 1]);
-            st_bytes32<ALIGN>(b, v);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = __float_as_uint(f[i]);
-            st_bytes32<ALIGN>(b, v);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = __float_as_uint(f[8 + i]);
-            st_bytes32<ALIGN>(b + 32, v);
+        for (int i = 0; i < W; i += ALIGN / 4) {
+            if (ALIGN == 32) ld_v8(v + i, b + 4 * i);
+            else ld_v4(v + i, b + 4 * i);
         }
         return;
     }
+    if (ALIGN == 0 && left >= 16) {
+        const uint32_t s = (uint32_t)reinterpret_cast<uintptr_t>(b) & 15u;
+        const uint8_t *f = b - s;
+        if (f >= span.first && f + 4 * W + 16 <= span.end) {
+            uint32_t w[W + 4];
+#pragma unroll
+            for (int i = 0; i < W + 4; i += 4) ld_v4(w + i, f + 4 * i);
+            shift_words<BF16, W>(w, s);
+#pragma unroll
+            for (int i = 0; i < W; ++i) v[i] = w[i];
+            return;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        if (BF16) {
+            const uint16_t *e = reinterpret_cast<const uint16_t *>(p);
+            v[i] = (2 * i < left ? (uint32_t)e[2 * i] : 0u) | (2 * i + 1 < left ? (uint32_t)e[2 * i + 1] << 16 : 0u);
+        } else {
+            v[i] = i < left ? reinterpret_cast<const uint32_t *>(p)[i] : 0u;
+        }
+    }
+}
+
+template <bool BF16>
+__device__ __forceinline__ void floats_of_words(float (&f)[16], const uint32_t (&v)[kRunWords<BF16>])
+{
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        f[i] = __uint_as_float(!BF16 ? v[i] : i & 1 ? v[i / 2] & 0xFFFF0000u : v[i / 2] << 16);
+}
+
+// Elements first .. last - 1 of a run.
+template <bool BF16>
+__device__ __forceinline__ void store_elements(uint8_t *b, const uint32_t (&v)[kRunWords<BF16>], int first, int last)
+{
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-        if (i >= left) continue;
-        if (BF16) reinterpret_cast<uint16_t *>(p)[i] = (uint16_t)bf16x2_of(f[i], 0.0f);
-        else reinterpret_cast<float *>(p)[i] = f[i];
+        if (i < first || i >= last) continue;
+        if (BF16) reinterpret_cast<uint16_t *>(b)[i] = (uint16_t)(i & 1 ? v[i / 2] >> 16 : v[i / 2]);
+        else reinterpret_cast<uint32_t *>(b)[i] = v[i];
     }
+}
+
+// A warp's runs: neighbouring lanes hold neighbouring runs of a row (run 0 starts a row), and all lanes call this, `left` <= 0
+// where there is nothing to store.  ALIGN 0: each lane stores the aligned vectors that begin in front of its run and so takes the end
+// of its left neighbour's; what has no neighbour to take it goes element by element.
+template <bool BF16, int ALIGN>
+__device__ __forceinline__ void store_run(void *p, const float (&f)[16], int64_t left, int64_t run)
+{
+    constexpr int W = kRunWords<BF16>;
+    uint8_t *b = reinterpret_cast<uint8_t *>(p);
+    uint32_t v[W];
+#pragma unroll
+    for (int i = 0; i < W; ++i) v[i] = BF16 ? bf16x2_of(f[2 * i % 16], f[(2 * i + 1) % 16]) : __float_as_uint(f[i]);
+    if (ALIGN >= 16) {
+        if (left >= 16) {
+#pragma unroll
+            for (int i = 0; i < W; i += ALIGN / 4) {
+                if (ALIGN == 32) st_v8(b + 4 * i, v + i);
+                else st_v4(b + 4 * i, v + i);
+            }
+        } else {
+            store_elements<BF16>(b, v, 0, (int)left);
+        }
+        return;
+    }
+    const int lane = threadIdx.x & 31;
+    uint32_t w[W + 4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __shfl_up_sync(0xFFFFFFFFu, v[W - 4 + i], 1);
+#pragma unroll
+    for (int i = 0; i < W; ++i) w[4 + i] = v[i];
+    const bool whole = left >= 16, next_whole = __shfl_down_sync(0xFFFFFFFFu, whole, 1), taken = lane < 31 && left > 16 && next_whole;
+    if (!whole) {
+        store_elements<BF16>(b, v, 0, (int)left);
+        return;
+    }
+    const uint32_t s = (uint32_t)reinterpret_cast<uintptr_t>(b) & 15u;
+    const int per = BF16 ? 2 : 4;
+    if (s == 0) {
+#pragma unroll
+        for (int i = 0; i < W; i += 4) st_v4(b + 4 * i, v + i);
+        return;
+    }
+    shift_words<BF16, W>(w, 16u - s);
+    if (lane > 0 && run > 0) st_v4(b - s, w);
+    else store_elements<BF16>(b, v, 0, (int)(16u - s) / per);
+#pragma unroll
+    for (int i = 4; i < W; i += 4) st_v4(b - s + 4 * i, w + i);
+    if (!taken) store_elements<BF16>(b, v, 16 - (int)s / per, 16);
 }
 
 // ---- blocks ------------------------------------------------------------------------------------
 
-// Largest magnitude of a run, as the bits of a non-negative float: NaN above infinity above every number.
-__device__ __forceinline__ uint32_t run_max_bits(const float (&f)[16])
+// Largest magnitude of a run, as the bits of a non-negative fp32: NaN above infinity above every number.
+template <bool BF16>
+__device__ __forceinline__ uint32_t run_max_bits(const uint32_t (&v)[kRunWords<BF16>])
 {
     uint32_t m = 0u;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) m = max(m, __float_as_uint(f[i]) & 0x7FFFFFFFu);
-    return m;
+    for (int i = 0; i < kRunWords<BF16>; ++i) m = BF16 ? __vmaxu2(m, v[i] & 0x7FFF7FFFu) : max(m, v[i] & 0x7FFFFFFFu);
+    return BF16 ? max(m & 0xFFFF0000u, m << 16) : m;
 }
 
 constexpr uint32_t kInfBits = 0x7F800000u;
@@ -225,38 +291,43 @@ __device__ __forceinline__ float float_of_e4m3(uint32_t code)
 // zeros needs no case of its own; NaN stays.
 __device__ __forceinline__ float nvfp4_largest(float m) { return m < 0x1p-100f ? 0x1p-100f : m; }
 
-// MXINT8 codes of a run: rint(x * 2^(6 - e)) clamped to +-127, as four words.
-__device__ __forceinline__ uint4 int8_codes(const float (&f)[16], float inv)
+// MXINT8 codes of a run: rint(x * 2^(6 - e)) clamped to +-127, as four words; code, max_bits: the block's e8m0 scale and its
+// largest magnitude.  The product with a power of two is exact, so that one fused multiply-add with 1.5 * 2^23 leaves the
+// rounded (to nearest even) value in the low byte; only a block whose largest magnitude rounds to 128 has to clamp.
+__device__ __forceinline__ uint4 int8_codes(float (&f)[16], uint32_t code, uint32_t max_bits)
 {
+    float mul = __uint_as_float((260u - code) << 23);       // 2^(133 - code)
+    if (code < 6u) {                                         // not a float; the elements are below 2^-120
+        mul = 0x1p127f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) f[i] = __fmul_rn(f[i], __uint_as_float((133u - code) << 23));
+    }
+    uint32_t b[16];
+    if ((max_bits & 0x7FFFFFu) < 0x7F0000u) {                // below 127.5 / 64 of its power of two
+#pragma unroll
+        for (int i = 0; i < 16; ++i) b[i] = __float_as_uint(__fmaf_rn(f[i], mul, 12582912.0f));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            b[i] = __float_as_uint(__fadd_rn(fminf(fmaxf(__fmul_rn(f[i], mul), -127.0f), 127.0f), 12582912.0f));
+    }
     uint32_t w[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        uint32_t b[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float z = __fmul_rn(__fmul_rn(f[4 * j + i], inv), 64.0f);
-            z = fminf(fmaxf(z, -127.0f), 127.0f);
-            b[i] = __float_as_uint(__fadd_rn(z, 12582912.0f));      // 1.5 * 2^23: to nearest even in the low byte
-        }
-        w[j] = prmt(prmt(b[0], b[1], 0x0040u), prmt(b[2], b[3], 0x0040u), 0x5410u);
-    }
+    for (int j = 0; j < 4; ++j) w[j] = prmt(prmt(b[4 * j], b[4 * j + 1], 0x0040u), prmt(b[4 * j + 2], b[4 * j + 3], 0x0040u), 0x5410u);
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
-// ... and back: q * 2^-6 * 2^e, exact (2^-133 at the smallest).
+// ... and back: q * 2^(e - 6), exact (2^-133 at the smallest).  Flipping its top bit makes a code q + 128, which in the low byte of 2^23 is
+// the float 2^23 + 128 + q.
 __device__ __forceinline__ void floats_of_int8(float (&f)[16], uint4 codes, uint32_t scale)
 {
-    const float s = pow2_of_code(scale);
+    float s = __uint_as_float((scale - 6u) << 23);
+    if (scale - 7u > 247u) s = __uint_as_float(scale == kNanE8M0 ? 0x7FC00000u : 0x00400000u >> (6u - scale));
     const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t u = w[j] ^ 0x80808080u;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int q = (int)(int8_t)(w[j] >> (8 * i));
-            f[4 * j + i] = __fmul_rn(__fmul_rn((float)q, 0.015625f), s);
-        }
-    if (scale == kNanE8M0) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(0x7FC00000u);
+        for (int i = 0; i < 4; ++i) f[4 * j + i] = __fmul_rn(__fadd_rn(__uint_as_float(prmt(u, 0x4B000000u, 0x7540u + i)), -8388736.0f), s);
     }
 }
 
@@ -274,19 +345,15 @@ __device__ __forceinline__ uint32_t gather_word(uint32_t code)
 // Runs of 16 elements, row by row, `per_row` of them; a warp's 32 lanes take neighbouring ones.  Row and run of a
 // thread are divided out once and then stepped.
 struct RunWalk {
-    int64_t row, run;
-    int64_t per_row, d_row, d_run;
-    __device__ RunWalk(int64_t first, int64_t stride, int64_t per_row_) : per_row(per_row_)
+    uint32_t row, run;
+    uint32_t per_row, d_row, d_run;
+    __device__ RunWalk(int64_t first, int64_t stride, uint32_t per_row_) : per_row(per_row_)
     {
-        if (((first | stride | per_row) >> 31) == 0) {       // 64-bit divisions cost a small launch 0.2 us
-            row = (uint32_t)first / (uint32_t)per_row;
-            d_row = (uint32_t)stride / (uint32_t)per_row;
-        } else {
-            row = first / per_row;
-            d_row = stride / per_row;
-        }
-        run = first - row * per_row;
-        d_run = stride - d_row * per_row;
+        if ((first >> 32) == 0) row = (uint32_t)first / per_row;       // a 64-bit division costs a small launch 0.2 us
+        else row = (uint32_t)(first / per_row);
+        d_row = (uint32_t)stride / per_row;
+        run = (uint32_t)first - row * per_row;
+        d_run = (uint32_t)stride - d_row * per_row;
     }
     __device__ void next()
     {

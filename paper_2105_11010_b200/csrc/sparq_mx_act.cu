@@ -17,8 +17,15 @@ namespace {
 constexpr float kGeluScale = 1.5957691216057308f;      // 2 sqrt(2 / pi)
 constexpr float kGeluCubic = 0.044715f;
 
-// 1 / (1 + exp(-z)); the approximate exponential and quotient are within a few units of 2^-24 of it.
-__device__ __forceinline__ float logistic(float z) { return __fdividef(1.0f, 1.0f + __expf(-z)); }
+// 1 / (1 + exp(-z)) from the approximate power of two (2 units of 2^-23) and reciprocal (1 unit).  What these flush to zero is lost
+// beside 1, or is a result below 2^-126.
+__device__ __forceinline__ float logistic(float z)
+{
+    float e, s;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(__fmul_rn(z, -1.4426950408889634f)));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(__fadd_rn(1.0f, e)));
+    return s;
+}
 
 template <int ACT>
 __device__ __forceinline__ float act_value(float x)
@@ -51,25 +58,28 @@ __device__ __forceinline__ void act_both(float x, float &y, float &d)
 }
 
 // Codes and scale of a run, its block's other half in the neighbouring lane.
-__device__ __forceinline__ void keep_run(const float (&f)[16], bool coded, int64_t row, int64_t run, int64_t pitch, int64_t words,
-                                         int8_t *codes, uint8_t *scales)
+template <bool BF16>
+__device__ __forceinline__ void keep_run(const uint32_t (&v)[kRunWords<BF16>], const float (&x)[16], bool coded, uint32_t row, uint32_t run, int64_t pitch,
+                                         int64_t words, int8_t *codes, uint8_t *scales)
 {
-    uint32_t mb = run_max_bits(f);
+    uint32_t mb = run_max_bits<BF16>(v);
     mb = max(mb, __shfl_xor_sync(0xFFFFFFFFu, mb, 1));
-    uint32_t code = e8m0_code(mb, 0u);
+    const uint32_t code = e8m0_code(mb, 0u);
     if (coded) {
-        const uint4 w = int8_codes(f, inv_pow2_of_code(code));
+        float f[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) f[j] = x[j];
+        const uint4 w = int8_codes(f, code, mb);
         reinterpret_cast<uint4 *>(codes + row * pitch)[run] = mb >= kInfBits ? make_uint4(0u, 0u, 0u, 0u) : w;
-    } else {
-        code = 0u;
     }
-    const uint32_t word = gather_word<8>(code);
+    const uint32_t word = gather_word<8>(coded ? code : 0u);
     if ((threadIdx.x & 7) == 0) *reinterpret_cast<uint32_t *>(scales + mx_scale_word<false>(row, run >> 3, words)) = word;
 }
 
 struct ActForward {
     const void *x, *up;
-    int64_t rows, cols, ldx, ldy, per_row;
+    int64_t rows, cols, ldx, ldy;
+    uint32_t per_row;
     void *y;
     int8_t *codes, *up_codes;
     uint8_t *scales, *up_scales;
@@ -85,21 +95,27 @@ act_forward_mx8_kernel(const ActForward g)
     RunWalk at(first, stride, g.per_row);
     dep_wait();
     dep_launch();
+    const Span sx = span_of<BF16>(g.x, g.rows, g.cols, g.ldx), su = span_of<BF16>(g.up, g.rows, g.cols, g.ldx);
     // per_row is a multiple of 32: a warp's lanes share a row and leave the loop together
     for (int64_t i = first; i < runs; i += stride, at.next()) {
-        const int64_t left = g.cols - at.run * 16, off = left > 0 ? (at.row * g.ldx + at.run * 16) * kWidth : 0;
-        const bool coded = at.run * 16 < pitch;
+        const int64_t left = g.cols - (int64_t)at.run * 16, off = left > 0 ? (at.row * g.ldx + at.run * 16) * kWidth : 0;
+        const bool coded = (int64_t)at.run * 16 < pitch;
+        uint32_t vx[kRunWords<BF16>], vu[kRunWords<BF16>];
+        load_words<BF16, ALIGN>(vx, reinterpret_cast<const uint8_t *>(g.x) + off, left, sx);
+        if (GATED) load_words<BF16, ALIGN>(vu, reinterpret_cast<const uint8_t *>(g.up) + off, left, su);
         float f[16], u[16];
-        load_run<BF16, ALIGN>(f, reinterpret_cast<const uint8_t *>(g.x) + off, left);
-        if (GATED) load_run<BF16, ALIGN>(u, reinterpret_cast<const uint8_t *>(g.up) + off, left);
-        keep_run(f, coded, at.row, at.run, pitch, words, g.codes, g.scales);
-        if (GATED) keep_run(u, coded, at.row, at.run, pitch, words, g.up_codes, g.up_scales);
+        floats_of_words<BF16>(f, vx);
+        keep_run<BF16>(vx, f, coded, at.row, at.run, pitch, words, g.codes, g.scales);
+        if (GATED) {
+            floats_of_words<BF16>(u, vu);
+            keep_run<BF16>(vu, u, coded, at.row, at.run, pitch, words, g.up_codes, g.up_scales);
+        }
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
             f[j] = act_value<ACT>(f[j]);
             if (GATED) f[j] = __fmul_rn(f[j], u[j]);
         }
-        if (left > 0) store_run<BF16, ALIGN>(reinterpret_cast<uint8_t *>(g.y) + (at.row * g.ldy + at.run * 16) * kWidth, f, left);
+        store_run<BF16, ALIGN>(reinterpret_cast<uint8_t *>(g.y) + (left > 0 ? (at.row * g.ldy + at.run * 16) * kWidth : 0), f, left, at.run);
     }
 }
 
@@ -107,7 +123,8 @@ struct ActBackward {
     const void *dy;
     const int8_t *codes, *up_codes;
     const uint8_t *scales, *up_scales;
-    int64_t rows, cols, lddy, lddx, per_row;
+    int64_t rows, cols, lddy, lddx;
+    uint32_t per_row;
     void *dx, *dup;
 };
 
@@ -121,27 +138,40 @@ act_backward_mx8_kernel(const ActBackward g)
     RunWalk at(first, stride, g.per_row);
     dep_wait();
     dep_launch();
-    for (int64_t i = first; i < runs; i += stride, at.next()) {
-        const int64_t left = g.cols - at.run * 16;
-        const int64_t sc = mx_scale_word<false>(at.row, at.run >> 3, words) + ((at.run >> 1) & 3);
-        float dy[16], x[16], u[16];
-        load_run<BF16, ALIGN>(dy, reinterpret_cast<const uint8_t *>(g.dy) + (at.row * g.lddy + at.run * 16) * kWidth, left);
-        const uint32_t scale = g.scales[sc];
-        floats_of_int8(x, reinterpret_cast<const uint4 *>(g.codes + at.row * pitch)[at.run], scale);
-        if (GATED) floats_of_int8(u, reinterpret_cast<const uint4 *>(g.up_codes + at.row * pitch)[at.run], g.up_scales[sc]);
-        const bool nan = scale == kNanE8M0;           // comparisons and minima would lose it
+    const Span sdy = span_of<BF16>(g.dy, g.rows, g.cols, g.lddy);
+    // a warp's lanes leave the loop together; those past the last run have nothing to store
+    for (int64_t i = first; i < ((runs + 31) & ~INT64_C(31)); i += stride, at.next()) {
+        float dx[16], u[16];
+        int64_t left = 0;
+        if (i < runs) {
+            left = g.cols - (int64_t)at.run * 16;
+            const int64_t sc = mx_scale_word<false>(at.row, at.run >> 3, words) + ((at.run >> 1) & 3);
+            uint32_t v[kRunWords<BF16>];
+            float x[16];
+            load_words<BF16, ALIGN>(v, reinterpret_cast<const uint8_t *>(g.dy) + (at.row * g.lddy + at.run * 16) * kWidth, left, sdy);
+            const uint32_t scale = g.scales[sc];
+            floats_of_int8(x, reinterpret_cast<const uint4 *>(g.codes + at.row * pitch)[at.run], scale);
+            if (GATED) floats_of_int8(u, reinterpret_cast<const uint4 *>(g.up_codes + at.row * pitch)[at.run], g.up_scales[sc]);
+            floats_of_words<BF16>(dx, v);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            float y, d;
-            act_both<ACT>(x[j], y, d);
-            if (nan) y = d = x[j];
-            const float t = dy[j];
-            dy[j] = __fmul_rn(GATED ? __fmul_rn(t, u[j]) : t, d);
-            if (GATED) u[j] = __fmul_rn(t, y);
+            for (int j = 0; j < 16; ++j) {
+                float y, d;
+                act_both<ACT>(x[j], y, d);
+                const float t = dx[j];
+                dx[j] = __fmul_rn(GATED ? __fmul_rn(t, u[j]) : t, d);
+                if (GATED) u[j] = __fmul_rn(t, y);
+            }
+            if (scale == kNanE8M0) {           // comparisons and minima lose it
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    dx[j] = x[j];
+                    if (GATED) u[j] = x[j];
+                }
+            }
         }
         const int64_t off = (at.row * g.lddx + at.run * 16) * kWidth;
-        store_run<BF16, ALIGN>(reinterpret_cast<uint8_t *>(g.dx) + off, dy, left);
-        if (GATED) store_run<BF16, ALIGN>(reinterpret_cast<uint8_t *>(g.dup) + off, u, left);
+        store_run<BF16, ALIGN>(reinterpret_cast<uint8_t *>(g.dx) + off, dx, left, at.run);
+        if (GATED) store_run<BF16, ALIGN>(reinterpret_cast<uint8_t *>(g.dup) + off, u, left, at.run);
     }
 }
 
@@ -159,10 +189,7 @@ int check_pitches(int dtype, int64_t rows, int64_t cols, int64_t lda, int64_t ld
     if (lda < cols || ldb < cols) return set_error(SPARQ_ERR_INVALID_ARG, "a leading dimension is less than the columns (%lld)", (long long)cols);
     if (values & (dtype == SPARQ_DTYPE_BF16 ? 1u : 3u)) return set_error(SPARQ_ERR_UNSUPPORTED, "a tensor is not aligned to its elements");
     if (kept & 15u) return set_error(SPARQ_ERR_UNSUPPORTED, "codes and scales must be 16-byte aligned");
-    const int64_t ld = lda > ldb ? lda : ldb;
-    if (rows > INT64_C(1) << 40 || ld > INT64_C(1) << 40 || (__int128)rows * (ld + 512) > INT64_C(1) << 60)
-        return set_error(SPARQ_ERR_UNSUPPORTED, "%lld rows of %lld elements are more than any device holds", (long long)rows, (long long)ld);
-    return SPARQ_OK;
+    return check_mx_extent(rows, cols, lda > ldb ? lda : ldb);
 }
 
 int min_align(int a, int b) { return a < b ? a : b; }
@@ -197,7 +224,7 @@ extern "C" int sparq_act_forward_mx8(const void *x, const void *up, int dtype, i
     const bool bf16 = dtype == SPARQ_DTYPE_BF16;
     const int width = bf16 ? 2 : 4;
     const int align = min_align(min_align(run_align(x, ldx, width), run_align(y, ldy, width)), up ? run_align(up, ldx, width) : 32);
-    const ActForward g = {x, up, rows, cols, ldx, ldy, 2 * mx_scale_cols(SPARQ_MXINT8, cols), y, codes, up_codes, scales, up_scales};
+    const ActForward g = {x, up, rows, cols, ldx, ldy, (uint32_t)(2 * mx_scale_cols(SPARQ_MXINT8, cols)), y, codes, up_codes, scales, up_scales};
     int blocks = 0;
     if ((rc = run_grid(rows * g.per_row, &blocks)) != SPARQ_OK) return rc;
     const auto kernel = SPARQ_ACT_PICK(act_forward_mx8_kernel, bf16, align, act, up != nullptr);
@@ -219,7 +246,7 @@ extern "C" int sparq_act_backward_mx8(const void *dy, int dtype, int64_t rows, i
     const bool bf16 = dtype == SPARQ_DTYPE_BF16;
     const int width = bf16 ? 2 : 4;
     const int align = min_align(min_align(run_align(dy, lddy, width), run_align(dx, lddx, width)), dup ? run_align(dup, lddx, width) : 32);
-    const ActBackward g = {dy, codes, up_codes, scales, up_scales, rows, cols, lddy, lddx, (cols + 15) / 16, dx, dup};
+    const ActBackward g = {dy, codes, up_codes, scales, up_scales, rows, cols, lddy, lddx, (uint32_t)((cols + 15) / 16), dx, dup};
     int blocks = 0;
     if ((rc = run_grid(rows * g.per_row, &blocks)) != SPARQ_OK) return rc;
     const auto kernel = SPARQ_ACT_PICK(act_backward_mx8_kernel, bf16, align, act, dup != nullptr);

@@ -22,7 +22,7 @@ def test_sizes(fmt, rows, cols):
 
 def test_sizes_refuse():
     for f in (sparq.sparq_mx_code_bytes, sparq.sparq_mx_scale_bytes):
-        for args, code in (((3, 1, 1), -1), ((-1, 1, 1), -1), ((0, -1, 1), -1), ((0, 1, -1), -1), ((0, 1 << 41, 1), -2), ((0, 1 << 40, 1 << 40), -2)):
+        for args, code in (((3, 1, 1), -1), ((-1, 1, 1), -1), ((0, -1, 1), -1), ((0, 1, -1), -1), ((0, 1 << 41, 1), -2), ((0, 1, (1 << 31) - 255), -2), ((0, (1 << 31) - 257, (1 << 31) - 257), -2)):
             with pytest.raises(sparq.SparqError) as e:
                 f(*args)
             assert e.value.code == code, args
@@ -54,7 +54,7 @@ def test_codec(quantize):
     refused(-2, "aligned", call(dtype=1, x=P + 1))
     refused(-2, "aligned", call(codes=P + 8))
     refused(-2, "aligned", call(scales=P + 4))
-    refused(-2, "more than any device", call(rows=1 << 41))
+    refused(-2, "2^31", call(rows=1 << 41))
     refused(-2, "more than any device", call(rows=1 << 30, ld=1 << 35))
     assert call(rows=0, x=None, codes=None, scales=None) == 0 and call(cols=0, ld=0, x=None, codes=None, scales=None) == 0
 
@@ -106,7 +106,7 @@ def test_act(forward):
     refused(-2, "aligned", call(y=P + 2))
     refused(-2, "aligned", call(codes=P + 8))
     refused(-2, "aligned", call(up=P, uc=P, us=P + 1))
-    refused(-2, "more than any device", call(rows=1 << 41))
+    refused(-2, "2^31", call(rows=1 << 41))
     assert call(rows=0, x=None) == 0 and call(cols=0, x=None) == 0
 
 
