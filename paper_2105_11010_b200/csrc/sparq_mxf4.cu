@@ -7,10 +7,10 @@ namespace {
 
 constexpr int kMxMaxDynSmem = 232448 - 4096;
 
-template <int BN, bool NV>
-cudaError_t launch_small(const CUtensorMap &map_b, const CUtensorMap &map_a, MxGemmArgs &g, int64_t grid, cudaStream_t st)
+template <int BN, bool NV, bool SWAP>
+cudaError_t launch_small(const CUtensorMap &map_a, const CUtensorMap &map_b, MxGemmArgs &g, int64_t grid, cudaStream_t st)
 {
-    auto kernel = sparq_mxf4_small_kernel<BN, NV>;
+    auto kernel = sparq_mxf4_small_kernel<BN, NV, SWAP>;
     static bool attr_set[64] = {};   // per device ordinal
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -20,17 +20,18 @@ cudaError_t launch_small(const CUtensorMap &map_b, const CUtensorMap &map_a, MxG
         if (e != cudaSuccess) return e;
         if (dev >= 0 && dev < 64) attr_set[dev] = true;
     }
-    const int recv = mx_recv_bytes(mx_own_groups(g.M < BN ? g.M : BN, g.split), g.split), stage = mx_small_stage(BN, NV);
+    const int64_t C = SWAP ? g.M : g.N;
+    const int recv = mx_recv_bytes(mx_own_groups(C < BN ? C : BN, g.split, SWAP), g.split, SWAP), stage = mx_small_stage(BN, NV);
     const int steps = (g.k_blocks + g.split - 1) / g.split, fit = (kMxMaxDynSmem - 1024 - recv) / stage;
     g.stages = steps < fit ? steps : fit;
     if (g.stages > kMaxStages) g.stages = kMaxStages;
-    return launch_overlapped_cluster(kernel, (int)grid, g.split, kMxSmallThreads, 1024 + g.stages * stage + recv, st, map_b, map_a, g);
+    return launch_overlapped_cluster(kernel, (int)grid, g.split, mx_small_threads(SWAP), 1024 + g.stages * stage + recv, st, map_a, map_b, g);
 }
 
-template <int BN>
-cudaError_t launch_small_of(bool nv, const CUtensorMap &map_b, const CUtensorMap &map_a, MxGemmArgs &g, int64_t grid, cudaStream_t st)
+template <int BN, bool SWAP>
+cudaError_t launch_small_of(bool nv, const CUtensorMap &map_a, const CUtensorMap &map_b, MxGemmArgs &g, int64_t grid, cudaStream_t st)
 {
-    return nv ? launch_small<BN, true>(map_b, map_a, g, grid, st) : launch_small<BN, false>(map_b, map_a, g, grid, st);
+    return nv ? launch_small<BN, true, SWAP>(map_a, map_b, g, grid, st) : launch_small<BN, false, SWAP>(map_a, map_b, g, grid, st);
 }
 
 template <bool NV>
@@ -115,17 +116,17 @@ extern "C" int sparq_gemm_mxf4(const void *A, const uint8_t *A_scales, const voi
         const cudaError_t ce = nv ? launch_pair<true>(map, p, st) : launch_pair<false>(map, p, st);
         return ce == cudaSuccess ? SPARQ_OK : cuda_error(ce, "sparq_mxf4_kernel launch");
     }
-    const int bn = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
-    const int64_t tiles = (M + bn - 1) / bn * ((N + 127) / 128);
+    const bool swap = M <= 32;
+    const int bn = M <= 16 ? 16 : M <= 32 ? 32 : 128;
+    const int64_t tiles = (swap ? 1 : (M + 127) / 128) * ((N + 127) / 128);
     g.split = 1;
     while (g.split < 8 && tiles * g.split * 2 <= sms && g.k_blocks >= 2 * g.split) g.split *= 2;
     if (tiles * g.split > INT64_C(2147483647)) return set_error(SPARQ_ERR_UNSUPPORTED, "more than 2^31 tiles");
     CUtensorMap map_a, map_b;
-    if ((rc = encode_matrix(&map_a, CU_TENSOR_MAP_DATA_TYPE_UINT8, A, pitch, M, pitch, kMxBK, bn, CU_TENSOR_MAP_SWIZZLE_128B)) != SPARQ_OK) return rc;
+    if ((rc = encode_matrix(&map_a, CU_TENSOR_MAP_DATA_TYPE_UINT8, A, pitch, M, pitch, kMxBK, swap ? bn : 128, CU_TENSOR_MAP_SWIZZLE_128B)) != SPARQ_OK) return rc;
     if ((rc = encode_matrix(&map_b, CU_TENSOR_MAP_DATA_TYPE_UINT8, B, pitch, N, pitch, kMxBK, 128, CU_TENSOR_MAP_SWIZZLE_128B)) != SPARQ_OK) return rc;
     const int64_t grid = tiles * g.split;
-    const cudaError_t ce = bn == 16 ? launch_small_of<16>(nv, map_b, map_a, g, grid, st)
-                         : bn == 32 ? launch_small_of<32>(nv, map_b, map_a, g, grid, st)
-                         : bn == 64 ? launch_small_of<64>(nv, map_b, map_a, g, grid, st) : launch_small_of<128>(nv, map_b, map_a, g, grid, st);
+    const cudaError_t ce = bn == 16 ? launch_small_of<16, true>(nv, map_a, map_b, g, grid, st)
+                         : bn == 32 ? launch_small_of<32, true>(nv, map_a, map_b, g, grid, st) : launch_small_of<128, false>(nv, map_a, map_b, g, grid, st);
     return ce == cudaSuccess ? SPARQ_OK : cuda_error(ce, "sparq_mxf4_small_kernel launch");
 }

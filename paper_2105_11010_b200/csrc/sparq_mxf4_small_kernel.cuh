@@ -1,16 +1,20 @@
-// Products of 4-bit microscaled operands (sparq_gemm_mxf4) for few rows: tokens that are decoded, small batches.
+// Products of 4-bit microscaled operands (sparq_gemm_mxf4) for launches whose tiles all run at once: tokens that are decoded, small
+// batches.
 //
 //   out[m][n] = sum_k A[m][k] B[n][k]
 //
-// A tile is 128 rows of B (a layer's weights) x BN rows of A (tokens): the weights take the MMA's 128-row side, so that one
-// token costs one pass over the weights and BN = 16 columns of tensor memory.  Lane l of the accumulator is output column n0 + l, and
-// a warp's store of one token's outputs is contiguous.
+// A tile is 128 rows of one operand (the MMA's M side, accumulator lanes) x BN rows of the other (columns).
+//   SWAP     lanes are rows of B (a layer's weights), columns 16 or 32 rows of A: one token costs one pass over the weights and
+//            16 columns of tensor memory, and a warp's store of one token's outputs is contiguous.
+//   else     lanes are rows of A, columns 128 rows of B: a lane holds runs of an output row, stored 32 bytes at a time.
+//            (64 tokens as columns: 64 x 2048, K 512, 4.8 us, 128 tokens 7.2, most of it two-byte stores.)
 //
-// A cluster of `split` CTAs shares a tile where the tiles leave SMs idle: each takes an equal run of reduction
-// steps and sends its partial sums to the CTA that owns a token (groups of four) through distributed shared memory;
-// the owner adds them in rank order, so that the result does not depend on timing.
+// A cluster of `split` CTAs shares a tile where the tiles leave SMs idle: each takes an equal run of reduction steps
+// and sends its partial sums to the CTA that owns a group of columns through distributed shared memory; the owner adds
+// them in rank order, so that the result does not depend on timing.
 //
-// Warps: 0 producer, 1 tensor memory and MMA issue, 2..5 epilogue (lane quarter warp % 4).
+// Warps: 0 and the last producers (of either operand: one thread that issues all four copies of a step takes 0.35 us for it), 1 tensor
+// memory and MMA issue, the others epilogue (lane quarter warp % 4; of eight, every other 16 columns).
 #pragma once
 
 #include "sparq_mx_tc.cuh"
@@ -18,7 +22,7 @@
 namespace sparq {
 
 struct MxGemmArgs {
-    int64_t M, N;               // tokens, output columns
+    int64_t M, N;               // rows of A and of B
     int k_mmas, k_blocks;       // reduction steps of 64 and of 256 elements
     int scale_tiles;            // tiles of a row block's scales in memory
     const uint8_t *a_scales, *b_scales;
@@ -31,8 +35,6 @@ struct MxGemmArgs {
     long long wait_limit;
     int stages, split;
 };
-
-constexpr int kMxSmallThreads = 192;
 
 __device__ __forceinline__ float mx_alpha(const MxGemmArgs &g)
 {
@@ -47,28 +49,33 @@ __device__ __forceinline__ float mx_finish(float acc, float alpha, float bias, i
     return y;
 }
 
-__host__ __device__ constexpr int mx_small_stage(int bn, bool nv) { return (128 + bn) * kMxBK + (1 + (bn + 127) / 128) * scale_tiles(nv) * kScaleTile; }
-// Groups of four tokens that each CTA of a cluster finishes, and its room for their partial sums.
-__host__ __device__ inline int mx_own_groups(int64_t tokens, int split) { return (int)((tokens + 3) / 4 + split - 1) / split; }
-__host__ __device__ inline int mx_recv_bytes(int groups, int split) { return split > 1 ? split * groups * 128 * 16 : 0; }
+__host__ __device__ constexpr int mx_small_epi(bool swap) { return swap ? 4 : 8; }
+__host__ __device__ constexpr int mx_small_threads(bool swap) { return 32 * (3 + mx_small_epi(swap)); }
+__host__ __device__ constexpr int mx_small_stage(int bn, bool nv) { return (128 + bn) * kMxBK + 2 * scale_tiles(nv) * kScaleTile; }
+// Columns that change hands together; groups that each CTA of a cluster finishes of a tile with `cols` columns, and its room
+// for their partial sums.
+__host__ __device__ constexpr int mx_group(bool swap) { return swap ? 4 : 16; }
+__host__ __device__ inline int mx_own_groups(int64_t cols, int split, bool swap) { return ((int)((cols + mx_group(swap) - 1) / mx_group(swap)) + split - 1) / split; }
+__host__ __device__ inline int mx_recv_bytes(int groups, int split, bool swap) { return split > 1 ? split * groups * mx_group(swap) * 128 * 4 : 0; }
 
-template <int BN, bool NV>
+template <int BN, bool NV, bool SWAP>
 struct Mxf4Small : MxCta {
-    static constexpr int T = scale_tiles(NV), kABlocks = (BN + 127) / 128;
-    static constexpr int kStage = mx_small_stage(BN, NV), kWeights = 128 * kMxBK, kTokens = BN * kMxBK;
-    static constexpr uint32_t kColsB = BN, kColsA = BN + 4 * T;       // columns of the scales, behind the accumulator's
-    static constexpr uint32_t kCols = tmem_columns(BN + 4 * T + 4 * T * kABlocks);
-    uint32_t recv, nt;
-    int64_t n0, m0;
-    int tokens, kb_first, groups, own, own_valid;
+    static constexpr int kEpi = mx_small_epi(SWAP), T = scale_tiles(NV), kGroup = mx_group(SWAP);
+    static constexpr int kStage = mx_small_stage(BN, NV), kRows = 128 * kMxBK, kScalesAt = (128 + BN) * kMxBK;
+    static constexpr uint32_t kColsR = BN, kColsC = BN + 4 * T;       // columns of the scales, behind the accumulator's
+    static constexpr uint32_t kCols = tmem_columns(BN + 8 * T);
+    uint32_t recv;
+    int64_t r0, c0;             // first row of either operand
+    int rows, cols, kb_first, groups, own, own_valid;
 
-    __device__ void produce(const CUtensorMap &map_b, const CUtensorMap &map_a, const MxGemmArgs &g) const
+    // The codes of one operand's rows and their scales (of whole blocks of 128 rows).
+    template <bool LANES>
+    __device__ void produce(const CUtensorMap &map, const uint8_t *scales, const MxGemmArgs &g) const
     {
         if (lane == 0) {
-            dep_launch();
-            const int64_t b_row = (int64_t)nt * g.scale_tiles * kScaleTile;
-            const int64_t a_row = m0 / 128 * g.scale_tiles * kScaleTile;
-            const int a_blocks = kABlocks == 2 && tokens > 128 ? 2 : 1;
+            if (LANES) dep_launch();
+            const int row = (int)(LANES ? r0 : c0);
+            const uint8_t *src = scales + (int64_t)(row / 128) * g.scale_tiles * kScaleTile;
             int it = 0, s = 0;
             uint32_t ph = 1;
             for (; it < steps; ++it) {
@@ -76,13 +83,9 @@ struct Mxf4Small : MxCta {
                 const uint32_t full = full_bar(s), at = smem + (uint32_t)(s * kStage);
                 const int kb = kb_first + it, t0 = kb * T;
                 const uint32_t sf = (uint32_t)(g.scale_tiles - t0 < T ? g.scale_tiles - t0 : T) * kScaleTile;
-                mbar_expect_tx(full, kWeights + kTokens + sf * (1 + a_blocks));
-                tma_load_2d(at, &map_b, full, kb * kMxBK, (int)n0);
-                tma_load_2d(at + kWeights, &map_a, full, kb * kMxBK, (int)m0);
-                tma_load_bytes(at + kWeights + kTokens, g.b_scales + b_row + (int64_t)t0 * kScaleTile, sf, full);
-                for (int b = 0; b < a_blocks; ++b)
-                    tma_load_bytes(at + kWeights + kTokens + (uint32_t)((1 + b) * T * kScaleTile),
-                                   g.a_scales + a_row + ((int64_t)b * g.scale_tiles + t0) * kScaleTile, sf, full);
+                mbar_expect_tx(full, (LANES ? kRows : BN * kMxBK) + sf);
+                tma_load_2d(at + (LANES ? 0 : kRows), &map, full, kb * kMxBK, row);
+                tma_load_bytes(at + kScalesAt + (LANES ? 0 : T * kScaleTile), src + (int64_t)t0 * kScaleTile, sf, full);
                 if (++s == S) { s = 0; ph ^= 1u; }
             }
             if (*abort_flag)       // none of this thread's copies may land after the CTA has exited
@@ -101,22 +104,19 @@ struct Mxf4Small : MxCta {
             mbar_wait(full_bar(s), ph, abort_flag, g.status, g.wait_limit);
             tc_fence_after();
             if (elected) {
-                const uint32_t at = smem + (uint32_t)(s * kStage), sf = at + kWeights + kTokens;
-                const int kb = kb_first + it, mmas = g.k_mmas - kb * kMxSteps < kMxSteps ? g.k_mmas - kb * kMxSteps : kMxSteps;
-                const uint64_t bdesc = make_smem_desc<kMxBK>(at), adesc = make_smem_desc<kMxBK>(at + kWeights);
+                const uint32_t at = smem + (uint32_t)(s * kStage), sf = at + kScalesAt;
+                const int mmas = g.k_mmas - (kb_first + it) * kMxSteps;
+                const uint64_t rdesc = make_smem_desc<kMxBK>(at), cdesc = make_smem_desc<kMxBK>(at + kRows);
 #pragma unroll
                 for (int k = 0; k < kMxSteps; ++k) {
                     if (k >= mmas) continue;
                     const int t = NV ? k : k >> 1;
                     if (NV || (k & 1) == 0) {
-                        tc_copy_scales(tmem + kColsB + 4 * t, scale_desc(sf + t * kScaleTile));
-#pragma unroll
-                        for (int b = 0; b < kABlocks; ++b)
-                            tc_copy_scales(tmem + kColsA + 4 * (kABlocks * t + b), scale_desc(sf + ((1 + b) * T + t) * kScaleTile));
+                        tc_copy_scales(tmem + kColsR + 4 * t, scale_desc(sf + t * kScaleTile));
+                        tc_copy_scales(tmem + kColsC + 4 * t, scale_desc(sf + (T + t) * kScaleTile));
                     }
-                    const uint32_t id = make_idesc_f4(BN, 128, NV, NV ? 0u : (k & 1) * 2u);
-                    tc_mma_f4<NV>(tmem, bdesc + (uint64_t)(k * 2), adesc + (uint64_t)(k * 2), id, tmem + kColsB + 4 * t,
-                                  tmem + kColsA + 4 * kABlocks * t, (it > 0 || k > 0) ? 1u : 0u);
+                    tc_mma_f4<NV>(tmem, rdesc + (uint64_t)(k * 2), cdesc + (uint64_t)(k * 2), make_idesc_f4(BN, 128, NV, NV ? 0u : (k & 1) * 2u),
+                                  tmem + kColsR + 4 * t, tmem + kColsC + 4 * t, (it > 0 || k > 0) ? 1u : 0u);
                 }
                 tc_commit(empty_bar(s));
             }
@@ -129,76 +129,129 @@ struct Mxf4Small : MxCta {
         __syncwarp();
     }
 
+    // kGroup columns of this lane from `col` on.  SWAP: the outputs of kGroup tokens, in columns of `out`; else a run of a row.
+    __device__ void put(const MxGemmArgs &g, int col, const float (&acc)[kGroup], float alpha, float lane_bias) const
+    {
+        const int r = (warp & 3) * 32 + lane;
+        if (r >= rows) return;
+        const int count = cols - col < kGroup ? cols - col : kGroup;
+        float y[kGroup];
+        if (SWAP) {
+#pragma unroll
+            for (int j = 0; j < kGroup; ++j) y[j] = mx_finish(acc[j], alpha, lane_bias, g.relu);
+            const int64_t at = (c0 + col) * g.N + r0 + r;
+            if (g.f32_out) {
+                float *f = g.f32_out + at;
+#pragma unroll
+                for (int j = 0; j < kGroup; ++j, f += g.N)
+                    if (j < count) *f = y[j];
+            }
+            if (g.bf16_out) {
+                uint16_t *h = g.bf16_out + at;
+#pragma unroll
+                for (int j = 0; j < kGroup; ++j, h += g.N)
+                    if (j < count) *h = (uint16_t)bf16x2_of(y[j], 0.0f);
+            }
+            return;
+        }
+        const int64_t n = c0 + col, at = (r0 + r) * g.N + n;
+#pragma unroll
+        for (int j = 0; j < kGroup; ++j) y[j] = mx_finish(acc[j], alpha, g.bias && j < count ? __ldg(g.bias + n + j) : 0.0f, g.relu);
+        if (g.f32_out) store_row<false>(g.f32_out + at, y, count);
+        if (g.bf16_out) store_row<true>(g.bf16_out + at, y, count);
+    }
+
+    template <bool BF16>
+    __device__ void store_row(void *out, const float (&y)[kGroup], int count) const
+    {
+        constexpr int W = BF16 ? kGroup / 2 : kGroup;
+        uint32_t v[W];
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[i] = BF16 ? bf16x2_of(y[2 * i % kGroup], y[(2 * i + 1) % kGroup]) : __float_as_uint(y[i]);
+        uint8_t *b = reinterpret_cast<uint8_t *>(out);
+        const uint32_t low = (uint32_t)reinterpret_cast<uintptr_t>(b);
+        if (count == kGroup && (low & 31u) == 0) {
+#pragma unroll
+            for (int i = 0; i < W; i += 8) st_v8(b + 4 * i, v + i);
+        } else if (count == kGroup && (low & 15u) == 0) {
+#pragma unroll
+            for (int i = 0; i < W; i += 4) st_v4(b + 4 * i, v + i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kGroup; ++i) {
+                if (i >= count) continue;
+                if (BF16) reinterpret_cast<uint16_t *>(b)[i] = (uint16_t)(v[i / 2 % W] >> (16 * (i & 1)));
+                else reinterpret_cast<uint32_t *>(b)[i] = v[i % W];
+            }
+        }
+    }
+
     __device__ void finish(const MxGemmArgs &g) const
     {
-        const int quarter = warp & 3;
-        const int64_t n = n0 + quarter * 32 + lane;
-        const bool live = n < g.N;
-        const float alpha = mx_alpha(g), bias = g.bias && live ? __ldg(g.bias + n) : 0.0f;
-        auto put = [&](int token, float acc) {
-            if (!live) return;
-            const float y = mx_finish(acc, alpha, bias, g.relu);
-            const int64_t at = (m0 + token) * g.N + n;
-            if (g.f32_out) g.f32_out[at] = y;
-            if (g.bf16_out) g.bf16_out[at] = (uint16_t)bf16x2_of(y, 0.0f);
-        };
+        const int quarter = warp & 3, half = (warp - 2) >> 2, r = quarter * 32 + lane;
+        const float alpha = mx_alpha(g), lane_bias = SWAP && g.bias && r < rows ? __ldg(g.bias + r0 + r) : 0.0f;
         mbar_wait(acc_bar(), 0, abort_flag, g.status, g.wait_limit);
         tc_fence_after();
         const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16);
-        constexpr int kChunk = BN < 32 ? 16 : 32;
         if (split > 1) {
             __syncwarp();
             cluster_wait();        // every CTA of the cluster has its barriers ready
         }
+        // partial sums: per rank and group, 16-byte pieces of all lanes one after the other
+        auto piece = [&](int from, int local, int q) { return recv + (uint32_t)((((from * own + local) * (kGroup / 4) + q) * 128 + r) * 16); };
 #pragma unroll 1
-        for (int c0 = 0; c0 < tokens; c0 += kChunk) {
+        for (int c = half * 16; c < cols; c += kEpi / 4 * 16) {
             uint32_t v[32];
-            if (kChunk == 32) tmem_ld_32x32_issue(taddr + c0, v);
-            else tmem_ld_32x16_issue(taddr + c0, v);
+            tmem_ld_32x16_issue(taddr + c, v);
             tmem_ld_wait();
-            if (split == 1) {
 #pragma unroll
-                for (int j = 0; j < kChunk; ++j)
-                    if (c0 + j < tokens) put(c0 + j, __uint_as_float(v[j]));
-            } else {
+            for (int i = 0; i < 16 / kGroup; ++i) {
+                const int col = c + kGroup * i;
+                if (col >= cols) continue;
+                if (split == 1) {
+                    float a[kGroup];
 #pragma unroll
-                for (int q = 0; q < kChunk / 4; ++q) {
-                    const int grp = c0 / 4 + q;
-                    if (grp >= groups) continue;
-                    const int owner = grp / own, local = grp - owner * own;
-                    const uint32_t dst = recv + (uint32_t)(((rank * own + local) * 128 + quarter * 32 + lane) * 16);
-                    store_remote16(map_to_rank(dst, owner), map_to_rank(recv_bar(), owner), v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+                    for (int j = 0; j < kGroup; ++j) a[j] = __uint_as_float(v[kGroup * i + j]);
+                    put(g, col, a, alpha, lane_bias);
+                } else if (r < rows) {
+                    const int grp = col / kGroup, owner = grp / own, local = grp - owner * own;
+                    const uint32_t bar = map_to_rank(recv_bar(), owner);
+#pragma unroll
+                    for (int q = 0; q < kGroup / 4; ++q) {
+                        const int e = kGroup * i + 4 * q;
+                        store_remote16(map_to_rank(piece(rank, local, q), owner), bar, v[e], v[e + 1], v[e + 2], v[e + 3]);
+                    }
                 }
             }
         }
         if (split > 1) {
             mbar_wait(recv_bar(), 0, abort_flag, g.status, g.wait_limit);
-            for (int local = 0; local < own_valid; ++local) {
-                float a[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                for (uint32_t q = 0; q < split; ++q) {
-                    uint4 p;
-                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(p.x), "=r"(p.y), "=r"(p.z), "=r"(p.w)
-                                 : "r"(recv + (uint32_t)((((int)q * own + local) * 128 + quarter * 32 + lane) * 16)));
-                    a[0] += __uint_as_float(p.x);
-                    a[1] += __uint_as_float(p.y);
-                    a[2] += __uint_as_float(p.z);
-                    a[3] += __uint_as_float(p.w);
-                }
-                const int token = (rank * own + local) * 4;
+#pragma unroll 1
+            for (int local = half; local < own_valid; local += kEpi / 4) {
+                float a[kGroup];
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (token + j < tokens) put(token + j, a[j]);
+                for (int j = 0; j < kGroup; ++j) a[j] = 0.0f;
+#pragma unroll 2
+                for (int from = 0; from < (int)split; ++from)
+#pragma unroll
+                    for (int q = 0; q < kGroup / 4; ++q) {
+                        uint32_t p[4];
+                        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(p[0]), "=r"(p[1]), "=r"(p[2]), "=r"(p[3]) : "r"(piece(from, local, q)));
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) a[4 * q + j] = __fadd_rn(a[4 * q + j], __uint_as_float(p[j]));
+                    }
+                put(g, (rank * own + local) * kGroup, a, alpha, lane_bias);
             }
         }
         tc_fence_before();
     }
 };
 
-template <int BN, bool NV>
-__global__ void __launch_bounds__(kMxSmallThreads)
-sparq_mxf4_small_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_a, const MxGemmArgs g)
+template <int BN, bool NV, bool SWAP>
+__global__ void __launch_bounds__(mx_small_threads(SWAP))
+sparq_mxf4_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const MxGemmArgs g)
 {
-    using Cta = Mxf4Small<BN, NV>;
+    using Cta = Mxf4Small<BN, NV, SWAP>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) MxBars bars;
     __shared__ uint32_t tmem_base_slot;
@@ -213,24 +266,25 @@ sparq_mxf4_small_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_
     c.recv = c.smem + (uint32_t)(c.S * Cta::kStage);
     const uint32_t split = c.split = (uint32_t)g.split, tile = blockIdx.x / split;
     c.rank = (int)(blockIdx.x - tile * split);
-    const uint32_t n_tiles = (uint32_t)((g.N + 127) / 128), mt = tile / n_tiles;
-    c.nt = tile - mt * n_tiles;
-    c.n0 = (int64_t)c.nt * 128;
-    c.m0 = (int64_t)mt * BN;
-    c.tokens = g.M - c.m0 < BN ? (int)(g.M - c.m0) : BN;
+    const int64_t R = SWAP ? g.N : g.M, C = SWAP ? g.M : g.N;
+    const uint32_t n_tiles = (uint32_t)((g.N + 127) / 128), mt = tile / n_tiles, nt = tile - mt * n_tiles;
+    c.r0 = (int64_t)(SWAP ? nt : mt) * 128;
+    c.c0 = (int64_t)(SWAP ? mt : nt) * BN;
+    c.rows = R - c.r0 < 128 ? (int)(R - c.r0) : 128;
+    c.cols = C - c.c0 < BN ? (int)(C - c.c0) : BN;
     c.kb_first = (int)((int64_t)c.rank * g.k_blocks / split);
     c.steps = (int)((int64_t)(c.rank + 1) * g.k_blocks / split) - c.kb_first;
-    c.groups = (c.tokens + 3) / 4;
-    c.own = mx_own_groups(c.tokens, (int)split);
+    c.groups = (c.cols + Cta::kGroup - 1) / Cta::kGroup;
+    c.own = mx_own_groups(c.cols, (int)split, SWAP);
     const int rest = c.groups - c.rank * c.own;
     c.own_valid = rest < 0 ? 0 : rest < c.own ? rest : c.own;
 
     if (warp == 0) {
         if (lane == 0) {
-            prefetch_tensormap(&map_b);
             prefetch_tensormap(&map_a);
+            prefetch_tensormap(&map_b);
             for (int s = 0; s < c.S; ++s) {
-                mbar_init(c.full_bar(s), 1);
+                mbar_init(c.full_bar(s), 2);
                 mbar_init(c.empty_bar(s), 1);
             }
             mbar_init(c.acc_bar(), 1);
@@ -248,17 +302,19 @@ sparq_mxf4_small_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_
     tc_fence_after();
     c.tmem = tmem_base_slot;
     if (split > 1) {
-        if (threadIdx.x == 0) mbar_expect_tx(c.recv_bar(), split * (uint32_t)c.own_valid * (128 * 16));
+        if (threadIdx.x == 0) mbar_expect_tx(c.recv_bar(), split * (uint32_t)(c.own_valid * c.rows) * (Cta::kGroup * 4));
         __syncwarp();
         cluster_arrive();       // "barriers ready": waited for before the first remote store
     }
     dep_wait();
+    constexpr int kLast = 2 + Cta::kEpi;
     switch (warp) {
-    case 0: c.produce(map_b, map_a, g); break;
+    case 0: c.template produce<true>(SWAP ? map_b : map_a, SWAP ? g.b_scales : g.a_scales, g); break;
     case 1: c.issue(g); break;
+    case kLast: c.template produce<false>(SWAP ? map_a : map_b, SWAP ? g.a_scales : g.b_scales, g); break;
     default: c.finish(g);
     }
-    if (split > 1 && warp < 2) {
+    if (split > 1 && (warp < 2 || warp == kLast)) {
         __syncwarp();
         cluster_wait();            // matches the arrival above
     }
