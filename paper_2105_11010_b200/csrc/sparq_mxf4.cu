@@ -8,7 +8,7 @@ namespace {
 constexpr int kMxMaxDynSmem = 232448 - 4096;
 
 template <int BN, bool NV, bool SWAP>
-cudaError_t launch_small(const CUtensorMap &map_a, const CUtensorMap &map_b, MxGemmArgs &g, int64_t grid, cudaStream_t st)
+cudaError_t launch_small(const CUtensorMap (&map)[6], MxGemmArgs &g, int64_t grid, cudaStream_t st)
 {
     auto kernel = sparq_mxf4_small_kernel<BN, NV, SWAP>;
     static bool attr_set[64] = {};   // per device ordinal
@@ -25,13 +25,13 @@ cudaError_t launch_small(const CUtensorMap &map_a, const CUtensorMap &map_b, MxG
     const int steps = (g.k_blocks + g.split - 1) / g.split, fit = (kMxMaxDynSmem - 1024 - recv) / stage;
     g.stages = steps < fit ? steps : fit;
     if (g.stages > kMaxStages) g.stages = kMaxStages;
-    return launch_overlapped_cluster(kernel, (int)grid, g.split, mx_small_threads(SWAP), 1024 + g.stages * stage + recv, st, map_a, map_b, g);
+    return launch_overlapped_cluster(kernel, (int)grid, g.split, mx_small_threads(SWAP), 1024 + g.stages * stage + recv, st, map[0], map[1], map[4], map[5], g);
 }
 
 template <int BN, bool SWAP>
-cudaError_t launch_small_of(bool nv, const CUtensorMap &map_a, const CUtensorMap &map_b, MxGemmArgs &g, int64_t grid, cudaStream_t st)
+cudaError_t launch_small_of(bool nv, const CUtensorMap (&map)[6], MxGemmArgs &g, int64_t grid, cudaStream_t st)
 {
-    return nv ? launch_small<BN, true, SWAP>(map_a, map_b, g, grid, st) : launch_small<BN, false, SWAP>(map_a, map_b, g, grid, st);
+    return nv ? launch_small<BN, true, SWAP>(map, g, grid, st) : launch_small<BN, false, SWAP>(map, g, grid, st);
 }
 
 template <bool NV>
@@ -49,6 +49,37 @@ cudaError_t launch_pair(const CUtensorMap (&map)[6], const MxPairArgs &p, cudaSt
         if (dev >= 0 && dev < 64) attr_set[dev] = true;
     }
     return launch_overlapped_cluster(kernel, 2 * p.pairs, 2, kPairThreads, smem, st, map[0], map[1], map[2], map[3], map[4], map[5], p);
+}
+
+struct Form {
+    int bn, split;          // 16 or 32: rows of A in columns; 128: rows of A in lanes; kPairTile: pairs
+    int64_t tiles;
+};
+
+// Clusters of 1, 2, 4 and 8 CTAs, one CTA on each SM, that run at once on an SM count like the B200's (148, 74, 33, 15: clusters stay
+// within a group of SMs).
+int clusters_at_once(int split, int sms) { return split == 1 ? sms : split == 2 ? sms / 2 : split == 4 ? sms * 33 / 148 : sms * 15 / 148; }
+
+// By estimates of the time in us, fitted to launches of 1 to 2048 rows, 512 to 8192 columns and K 512 to 8192 in every form (b:
+// reduction steps of 256 on a CTA; one token x 512 in one piece 2.5 / 4.1 / 10.4 us for 2 / 8 / 32 steps, 128 x 512 3.7 / 5.6 / 12.7, pairs
+// 5.3 / 7.0 / 13.6; split by eight 2.9 / 3.7 and 6.1 / 7.0 for 8 / 32).
+Form pick_form(int64_t M, int64_t N, int k_blocks, int sms)
+{
+    const int64_t n_tiles = (N + 127) / 128, pairs = ((M + kPairTile - 1) / kPairTile) * ((N + kPairTile - 1) / kPairTile);
+    const bool swap = M <= 32;
+    const int bn = M <= 16 ? 16 : M <= 32 ? 32 : 128;
+    Form best = {kPairTile, 1, pairs};
+    double cost = swap ? 1e30 : 3.2 + (double)((pairs + sms / 2 - 1) / (sms / 2)) * (1.5 + 0.28 * k_blocks);
+    const int64_t tiles = (swap ? 1 : (M + 127) / 128) * n_tiles;
+    for (int split = 1; split <= 8 && split <= k_blocks; split *= 2) {
+        const int64_t rounds = (tiles + clusters_at_once(split, sms) - 1) / clusters_at_once(split, sms);
+        const int b = (k_blocks + split - 1) / split;
+        double c = swap ? 1.95 + 0.26 * b : 3.1 + 0.3 * b;
+        if (split > 1) c += swap ? 0.5 : 0.7 + 1.8 * (double)(M < 128 ? M : 128) / 128;
+        c *= (double)rounds;
+        if (c < cost - 0.05) { cost = c; best = {bn, split, tiles}; }
+    }
+    return best;
 }
 
 }  // namespace
@@ -96,37 +127,35 @@ extern "C" int sparq_gemm_mxf4(const void *A, const uint8_t *A_scales, const voi
     g.wait_limit = kWaitLimitCycles;
     if ((rc = get_status_word(&g.status)) != SPARQ_OK) return rc;
 
+    g.staged = (N % (e->bf16_out ? 8 : 4)) == 0 && (((uintptr_t)e->f32_out | (uintptr_t)e->bf16_out) & 15u) == 0;
+
     const int64_t pitch = mx_code_pitch(format, K);
     cudaStream_t st = (cudaStream_t)stream;
-    const int64_t m_tiles = (M + kPairTile - 1) / kPairTile, n_tiles = (N + kPairTile - 1) / kPairTile;
-    if (m_tiles * n_tiles >= 16 && m_tiles * n_tiles <= INT64_C(1) << 30) {
-        MxPairArgs p = {g, (int)m_tiles, (int)n_tiles, 0, 0};
-        p.pairs = (int)(m_tiles * n_tiles < sms / 2 ? m_tiles * n_tiles : sms / 2);
-        p.staged = (N % (e->bf16_out ? 8 : 4)) == 0 && (((uintptr_t)e->f32_out | (uintptr_t)e->bf16_out) & 15u) == 0;
-        CUtensorMap map[6] = {};
-        if ((rc = encode_matrix(&map[0], CU_TENSOR_MAP_DATA_TYPE_UINT8, A, pitch, M, pitch, kMxBK, 128, CU_TENSOR_MAP_SWIZZLE_128B)) != SPARQ_OK ||
-            (rc = encode_matrix(&map[1], CU_TENSOR_MAP_DATA_TYPE_UINT8, B, pitch, N, pitch, kMxBK, 128, CU_TENSOR_MAP_SWIZZLE_128B)) != SPARQ_OK ||
-            (rc = encode_scale_tiles(&map[2], A_scales, g.scale_tiles, (M + 127) / 128, scale_tiles(nv), 1)) != SPARQ_OK ||
+    const Form form = pick_form(M, N, g.k_blocks, sms);
+    const int a_rows = form.bn < 128 ? form.bn : 128;
+    CUtensorMap map[6] = {};       // A, B, their scales (pairs), f32_out, bf16_out
+    if ((rc = encode_matrix(&map[0], CU_TENSOR_MAP_DATA_TYPE_UINT8, A, pitch, M, pitch, kMxBK, a_rows, CU_TENSOR_MAP_SWIZZLE_128B)) != SPARQ_OK ||
+        (rc = encode_matrix(&map[1], CU_TENSOR_MAP_DATA_TYPE_UINT8, B, pitch, N, pitch, kMxBK, 128, CU_TENSOR_MAP_SWIZZLE_128B)) != SPARQ_OK)
+        return rc;
+    if (g.staged && form.bn >= 128) {
+        if (e->f32_out &&
+            (rc = encode_matrix(&map[4], CU_TENSOR_MAP_DATA_TYPE_FLOAT32, e->f32_out, N, M, N * 4, 32, 32, CU_TENSOR_MAP_SWIZZLE_128B)) != SPARQ_OK) return rc;
+        if (e->bf16_out &&
+            (rc = encode_matrix(&map[5], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, e->bf16_out, N, M, N * 2, 64, 32, CU_TENSOR_MAP_SWIZZLE_128B)) != SPARQ_OK) return rc;
+    }
+    if (form.tiles * form.split > INT64_C(1) << 30) return set_error(SPARQ_ERR_UNSUPPORTED, "more than 2^30 tiles");
+    if (form.bn == kPairTile) {
+        MxPairArgs p = {g, (int)((M + kPairTile - 1) / kPairTile), (int)((N + kPairTile - 1) / kPairTile), 0};
+        p.pairs = (int)(form.tiles < sms / 2 ? form.tiles : sms / 2);
+        if ((rc = encode_scale_tiles(&map[2], A_scales, g.scale_tiles, (M + 127) / 128, scale_tiles(nv), 1)) != SPARQ_OK ||
             (rc = encode_scale_tiles(&map[3], B_scales, g.scale_tiles, (N + 127) / 128, scale_tiles(nv), 2)) != SPARQ_OK)
             return rc;
-        if (p.staged && e->f32_out &&
-            (rc = encode_matrix(&map[4], CU_TENSOR_MAP_DATA_TYPE_FLOAT32, e->f32_out, N, M, N * 4, 32, 32, CU_TENSOR_MAP_SWIZZLE_128B)) != SPARQ_OK) return rc;
-        if (p.staged && e->bf16_out &&
-            (rc = encode_matrix(&map[5], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, e->bf16_out, N, M, N * 2, 64, 32, CU_TENSOR_MAP_SWIZZLE_128B)) != SPARQ_OK) return rc;
         const cudaError_t ce = nv ? launch_pair<true>(map, p, st) : launch_pair<false>(map, p, st);
         return ce == cudaSuccess ? SPARQ_OK : cuda_error(ce, "sparq_mxf4_kernel launch");
     }
-    const bool swap = M <= 32;
-    const int bn = M <= 16 ? 16 : M <= 32 ? 32 : 128;
-    const int64_t tiles = (swap ? 1 : (M + 127) / 128) * ((N + 127) / 128);
-    g.split = 1;
-    while (g.split < 8 && tiles * g.split * 2 <= sms && g.k_blocks >= 2 * g.split) g.split *= 2;
-    if (tiles * g.split > INT64_C(2147483647)) return set_error(SPARQ_ERR_UNSUPPORTED, "more than 2^31 tiles");
-    CUtensorMap map_a, map_b;
-    if ((rc = encode_matrix(&map_a, CU_TENSOR_MAP_DATA_TYPE_UINT8, A, pitch, M, pitch, kMxBK, swap ? bn : 128, CU_TENSOR_MAP_SWIZZLE_128B)) != SPARQ_OK) return rc;
-    if ((rc = encode_matrix(&map_b, CU_TENSOR_MAP_DATA_TYPE_UINT8, B, pitch, N, pitch, kMxBK, 128, CU_TENSOR_MAP_SWIZZLE_128B)) != SPARQ_OK) return rc;
-    const int64_t grid = tiles * g.split;
-    const cudaError_t ce = bn == 16 ? launch_small_of<16, true>(nv, map_a, map_b, g, grid, st)
-                         : bn == 32 ? launch_small_of<32, true>(nv, map_a, map_b, g, grid, st) : launch_small_of<128, false>(nv, map_a, map_b, g, grid, st);
+    g.split = form.split;
+    const int64_t grid = form.tiles * form.split;
+    const cudaError_t ce = form.bn == 16 ? launch_small_of<16, true>(nv, map, g, grid, st)
+                         : form.bn == 32 ? launch_small_of<32, true>(nv, map, g, grid, st) : launch_small_of<128, false>(nv, map, g, grid, st);
     return ce == cudaSuccess ? SPARQ_OK : cuda_error(ce, "sparq_mxf4_small_kernel launch");
 }

@@ -28,14 +28,12 @@ constexpr uint32_t kPairScales = 464;           // first column of the scales
 __host__ __device__ constexpr int pair_stage(bool nv) { return 2 * 128 * kMxBK + 3 * scale_tiles(nv) * kScaleTile; }
 // Stages start on 1024-byte boundaries.
 __host__ __device__ constexpr int pair_stage_room(bool nv) { return (pair_stage(nv) + 1023) / 1024 * 1024; }
-constexpr int kPairStaging = 32 * 128;          // per epilogue warp: 32 rows of a box
-__host__ __device__ constexpr int pair_stages(bool nv) { return (232448 - 1024 - 512 - kPairEpiWarps * kPairStaging) / pair_stage_room(nv); }
-__host__ __device__ constexpr int pair_smem(bool nv) { return 1024 + pair_stages(nv) * pair_stage_room(nv) + kPairEpiWarps * kPairStaging; }
+__host__ __device__ constexpr int pair_stages(bool nv) { return (232448 - 1024 - 512 - kPairEpiWarps * kMxStaging) / pair_stage_room(nv); }
+__host__ __device__ constexpr int pair_smem(bool nv) { return 1024 + pair_stages(nv) * pair_stage_room(nv) + kPairEpiWarps * kMxStaging; }
 
 struct MxPairArgs {
     MxGemmArgs g;
     int m_tiles, n_tiles, pairs;
-    int staged;                 // outputs go out through shared memory, in boxes
 };
 
 // Tile t in an order that keeps eight rows of tiles together: their operands and the column's stay in L2.
@@ -139,86 +137,6 @@ struct Mxf4Pair : MxCta {
         __syncwarp();
     }
 
-    // Scaling, bias and ReLU of C columns of a row.
-    template <int C>
-    __device__ void finish_row(const MxGemmArgs &g, float (&y)[C], int64_t n, float alpha) const
-    {
-#pragma unroll
-        for (int j = 0; j < C; ++j) y[j] = __fmul_rn(y[j], alpha);
-        if (g.bias) {
-            if (n + C <= g.N && (reinterpret_cast<uintptr_t>(g.bias + n) & 15u) == 0) {
-#pragma unroll
-                for (int j = 0; j < C; j += 4) {
-                    const float4 b = __ldg(reinterpret_cast<const float4 *>(g.bias + n + j));
-                    y[j] = __fadd_rn(y[j], b.x);
-                    y[j + 1] = __fadd_rn(y[j + 1], b.y);
-                    y[j + 2] = __fadd_rn(y[j + 2], b.z);
-                    y[j + 3] = __fadd_rn(y[j + 3], b.w);
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < C; ++j) y[j] = __fadd_rn(y[j], n + j < g.N ? __ldg(g.bias + n + j) : 0.0f);
-            }
-        }
-        if (g.relu) {
-#pragma unroll
-            for (int j = 0; j < C; ++j) y[j] = y[j] > 0.0f ? y[j] : 0.0f;
-        }
-    }
-
-    // 32 rows x 128 bytes of one output through this warp's staging memory (rows of 128 bytes, swizzled as TMA does).
-    __device__ void store_box(const CUtensorMap &map, const uint32_t (&w)[32], uint32_t stage, int64_t m, int64_t n, const MxGemmArgs &g) const
-    {
-        if (lane == 0) tma_store_wait_read<0>();        // the box before has left
-        __syncwarp();
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" :: "r"(stage + (uint32_t)(lane * 128 + ((j ^ (lane & 7)) << 4))), "r"(w[4 * j]),
-                         "r"(w[4 * j + 1]), "r"(w[4 * j + 2]), "r"(w[4 * j + 3]) : "memory");
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0 && m < g.M && n < g.N) {
-            tma_store_2d(&map, stage, (int)n, (int)m);
-            tma_store_commit();
-        }
-    }
-
-    // 64 columns of 32 rows.  STAGED: rows of outputs start on 16-byte boundaries.
-    template <bool STAGED>
-    __device__ void put_span(const CUtensorMap &map_f, const CUtensorMap &map_h, const MxGemmArgs &g, const uint32_t (&v)[2][32], int64_t m0, int64_t n,
-                             float alpha) const
-    {
-        const uint32_t stage = smem + (uint32_t)(kStages * kRoom + (warp - 2) * kPairStaging);
-        uint32_t h[32];
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            float y[32];
-#pragma unroll
-            for (int j = 0; j < 32; ++j) y[j] = __uint_as_float(v[q][j]);
-            finish_row<32>(g, y, n + 32 * q, alpha);
-            if (STAGED) {
-                if (g.f32_out) {
-                    uint32_t f[32];
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) f[j] = __float_as_uint(y[j]);
-                    store_box(map_f, f, stage, m0, n + 32 * q, g);
-                }
-#pragma unroll
-                for (int j = 0; j < 16; ++j) h[16 * q + j] = bf16x2_of(y[2 * j], y[2 * j + 1]);
-            } else if (m0 + lane < g.M) {
-                // a row's pieces, element by element
-                const int64_t at = (m0 + lane) * g.N + n + 32 * q;
-#pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    if (n + 32 * q + j >= g.N) continue;
-                    if (g.f32_out) g.f32_out[at + j] = y[j];
-                    if (g.bf16_out) g.bf16_out[at + j] = (uint16_t)bf16x2_of(y[j], 0.0f);
-                }
-            }
-        }
-        if (STAGED && g.bf16_out) store_box(map_h, h, stage, m0, n, g);
-    }
-
     __device__ void finish(const CUtensorMap &map_f, const CUtensorMap &map_h, const MxPairArgs &p) const
     {
         const MxGemmArgs &g = p.g;
@@ -248,8 +166,7 @@ struct Mxf4Pair : MxCta {
                     __syncwarp();
                     if (lane == 0) mbar_arrive_remote(freed);
                 }
-                if (p.staged) put_span<true>(map_f, map_h, g, v, m0, n0 + span * 64, alpha);
-                else put_span<false>(map_f, map_h, g, v, m0, n0 + span * 64, alpha);
+                mx_put_span(map_f, map_h, g, v, smem + (uint32_t)(kStages * kRoom + (warp - 2) * kMxStaging), m0, n0 + span * 64, alpha);
             }
         }
         if (lane == 0) tma_store_wait_all();

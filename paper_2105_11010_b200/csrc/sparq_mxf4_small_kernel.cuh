@@ -34,6 +34,7 @@ struct MxGemmArgs {
     unsigned int *status;
     long long wait_limit;
     int stages, split;
+    int staged;                 // outputs go out through shared memory, in boxes: their rows start on 16-byte boundaries
 };
 
 __device__ __forceinline__ float mx_alpha(const MxGemmArgs &g)
@@ -47,6 +48,117 @@ __device__ __forceinline__ float mx_finish(float acc, float alpha, float bias, i
     float y = __fadd_rn(__fmul_rn(acc, alpha), bias);
     if (relu) y = y > 0.0f ? y : 0.0f;
     return y;
+}
+
+// 32 columns of an output row from their accumulators.
+__device__ __forceinline__ void mx_finish_row(const MxGemmArgs &g, float (&y)[32], const uint32_t (&v)[32], int64_t n, float alpha)
+{
+#pragma unroll
+    for (int j = 0; j < 32; ++j) y[j] = __fmul_rn(__uint_as_float(v[j]), alpha);
+    if (g.bias) {
+        if (n + 32 <= g.N && (reinterpret_cast<uintptr_t>(g.bias + n) & 15u) == 0) {
+#pragma unroll
+            for (int j = 0; j < 32; j += 4) {
+                const float4 b = __ldg(reinterpret_cast<const float4 *>(g.bias + n + j));
+                y[j] = __fadd_rn(y[j], b.x);
+                y[j + 1] = __fadd_rn(y[j + 1], b.y);
+                y[j + 2] = __fadd_rn(y[j + 2], b.z);
+                y[j + 3] = __fadd_rn(y[j + 3], b.w);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) y[j] = __fadd_rn(y[j], n + j < g.N ? __ldg(g.bias + n + j) : 0.0f);
+        }
+    }
+    if (g.relu) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) y[j] = y[j] > 0.0f ? y[j] : 0.0f;
+    }
+}
+
+// 32 rows x 128 bytes of one output through a warp's staging memory (rows of 128 bytes, swizzled as TMA does).  Rows of 32 lanes
+// stored straight from registers are 32 lines to an instruction: 128 x 512, K 512, 5.3 us.
+constexpr int kMxStaging = 32 * 128;
+__device__ __forceinline__ void mx_stage_row(const uint32_t (&w)[32], uint32_t stage)
+{
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" :: "r"(stage + (uint32_t)(lane * 128 + ((j ^ (lane & 7)) << 4))), "r"(w[4 * j]),
+                     "r"(w[4 * j + 1]), "r"(w[4 * j + 2]), "r"(w[4 * j + 3]) : "memory");
+}
+__device__ __forceinline__ void mx_store_box(const CUtensorMap &map, const uint32_t (&w)[32], uint32_t stage, int64_t m, int64_t n, const MxGemmArgs &g)
+{
+    const int lane = threadIdx.x & 31;
+    if (lane == 0) tma_store_wait_read<0>();        // the box before has left
+    __syncwarp();
+    mx_stage_row(w, stage);
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0 && m < g.M && n < g.N) {
+        tma_store_2d(&map, stage, (int)n, (int)m);
+        tma_store_commit();
+    }
+}
+// The same for rows that TMA cannot address (odd lengths): the warp stores one row after the other, lane by lane.
+template <bool BF16>
+__device__ __forceinline__ void mx_store_rows(void *out, const uint32_t (&w)[32], uint32_t stage, int64_t m, int64_t n, const MxGemmArgs &g)
+{
+    const int lane = threadIdx.x & 31, col = BF16 ? 2 * lane : lane;
+    __syncwarp();
+    mx_stage_row(w, stage);
+    __syncwarp();
+    const int rows = g.M - m < 32 ? (int)(g.M - m) : 32, cols = g.N - n - col < 2 ? (int)(g.N - n - col) : 2;
+    const uint32_t src = stage + (uint32_t)((lane & 3) * 4);
+    const int64_t at = m * g.N + n + col;
+    if (BF16) {
+        uint16_t *h = reinterpret_cast<uint16_t *>(out) + at;
+        const bool pairs = (g.N & 1) == 0 && (reinterpret_cast<uintptr_t>(h) & 3u) == 0;
+#pragma unroll 4
+        for (int r = 0; r < rows; ++r, h += g.N) {
+            uint32_t v;
+            asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(src + (uint32_t)(r * 128 + (((lane >> 2) ^ (r & 7)) << 4))));
+            if (cols == 2 && pairs) {
+                *reinterpret_cast<uint32_t *>(h) = v;
+            } else {
+                if (cols > 0) h[0] = (uint16_t)v;
+                if (cols > 1) h[1] = (uint16_t)(v >> 16);
+            }
+        }
+    } else {
+        uint32_t *f = reinterpret_cast<uint32_t *>(out) + at;
+#pragma unroll 4
+        for (int r = 0; r < rows; ++r, f += g.N) {
+            uint32_t v;
+            asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(src + (uint32_t)(r * 128 + (((lane >> 2) ^ (r & 7)) << 4))));
+            if (cols > 0) *f = v;
+        }
+    }
+}
+
+// 64 columns of a warp's 32 rows: row m0 + lane, columns n .. n + 63 from v.
+__device__ __forceinline__ void mx_put_span(const CUtensorMap &map_f, const CUtensorMap &map_h, const MxGemmArgs &g, const uint32_t (&v)[2][32],
+                                            uint32_t stage, int64_t m0, int64_t n, float alpha)
+{
+    uint32_t h[32];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        float y[32];
+        mx_finish_row(g, y, v[q], n + 32 * q, alpha);
+        if (g.f32_out) {
+            uint32_t f[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) f[j] = __float_as_uint(y[j]);
+            if (g.staged) mx_store_box(map_f, f, stage, m0, n + 32 * q, g);
+            else mx_store_rows<false>(g.f32_out, f, stage, m0, n + 32 * q, g);
+        }
+#pragma unroll
+        for (int j = 0; j < 16; ++j) h[16 * q + j] = bf16x2_of(y[2 * j], y[2 * j + 1]);
+    }
+    if (g.bf16_out) {
+        if (g.staged) mx_store_box(map_h, h, stage, m0, n, g);
+        else mx_store_rows<true>(g.bf16_out, h, stage, m0, n, g);
+    }
 }
 
 __host__ __device__ constexpr int mx_small_epi(bool swap) { return swap ? 4 : 8; }
@@ -186,7 +298,7 @@ struct Mxf4Small : MxCta {
         }
     }
 
-    __device__ void finish(const MxGemmArgs &g) const
+    __device__ void finish(const CUtensorMap &map_f, const CUtensorMap &map_h, const MxGemmArgs &g) const
     {
         const int quarter = warp & 3, half = (warp - 2) >> 2, r = quarter * 32 + lane;
         const float alpha = mx_alpha(g), lane_bias = SWAP && g.bias && r < rows ? __ldg(g.bias + r0 + r) : 0.0f;
@@ -196,6 +308,19 @@ struct Mxf4Small : MxCta {
         if (split > 1) {
             __syncwarp();
             cluster_wait();        // every CTA of the cluster has its barriers ready
+        }
+        if (!SWAP && split == 1) {     // 64 columns to a warp; the ring is free, its last MMA has read it
+            if (half * 64 < cols) {
+                uint32_t v[2][32];
+                tmem_ld_32x32_issue(taddr + half * 64, v[0]);
+                tmem_ld_32x32_issue(taddr + half * 64 + 32, v[1]);
+                tmem_ld_wait();
+                mx_put_span(map_f, map_h, g, v, smem + (uint32_t)((warp - 2) * kMxStaging), r0 + quarter * 32, c0 + half * 64, alpha);
+                if (lane == 0) tma_store_wait_all();
+                __syncwarp();
+            }
+            tc_fence_before();
+            return;
         }
         // partial sums: per rank and group, 16-byte pieces of all lanes one after the other
         auto piece = [&](int from, int local, int q) { return recv + (uint32_t)((((from * own + local) * (kGroup / 4) + q) * 128 + r) * 16); };
@@ -249,7 +374,8 @@ struct Mxf4Small : MxCta {
 
 template <int BN, bool NV, bool SWAP>
 __global__ void __launch_bounds__(mx_small_threads(SWAP))
-sparq_mxf4_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const MxGemmArgs g)
+sparq_mxf4_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_f,
+                        const __grid_constant__ CUtensorMap map_h, const MxGemmArgs g)
 {
     using Cta = Mxf4Small<BN, NV, SWAP>;
     extern __shared__ uint8_t smem_raw[];
@@ -312,7 +438,7 @@ sparq_mxf4_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_
     case 0: c.template produce<true>(SWAP ? map_b : map_a, SWAP ? g.b_scales : g.a_scales, g); break;
     case 1: c.issue(g); break;
     case kLast: c.template produce<false>(SWAP ? map_a : map_b, SWAP ? g.a_scales : g.b_scales, g); break;
-    default: c.finish(g);
+    default: c.finish(map_f, map_h, g);
     }
     if (split > 1 && (warp < 2 || warp == kLast)) {
         __syncwarp();
