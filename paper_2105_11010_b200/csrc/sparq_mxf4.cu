@@ -56,10 +56,6 @@ struct Form {
     int64_t tiles;
 };
 
-// Clusters of 1, 2, 4 and 8 CTAs, one CTA on each SM, that run at once on an SM count like the B200's (148, 74, 33, 15: clusters stay
-// within a group of SMs).
-int clusters_at_once(int split, int sms) { return split == 1 ? sms : split == 2 ? sms / 2 : split == 4 ? sms * 33 / 148 : sms * 15 / 148; }
-
 // By estimates of the time in us, fitted to launches of 1 to 2048 rows, 512 to 8192 columns and K 512 to 8192 in every form (b:
 // reduction steps of 256 on a CTA; one token x 512 in one piece 2.5 / 4.1 / 10.4 us for 2 / 8 / 32 steps, 128 x 512 3.7 / 5.6 / 12.7, pairs
 // 5.3 / 7.0 / 13.6; split by eight 2.9 / 3.7 and 6.1 / 7.0 for 8 / 32).

@@ -90,7 +90,7 @@ extern "C" int sparq_wgrad_mx8(const void *dy, int64_t lddy, const int8_t *codes
     }
     const int64_t tiles = (N + 127) / 128 * ((K + kWgBN - 1) / kWgBN);
     g.split = 1;
-    while (g.split < 8 && tiles * g.split * 2 <= sms && g.blocks >= 4 * g.split) g.split *= 2;
+    while (g.split < 8 && tiles <= clusters_at_once(2 * g.split, sms) && g.blocks >= 2 * g.split) g.split *= 2;
     g.stages = kWgStages;
     if (tiles * g.split > INT64_C(2147483647)) return set_error(SPARQ_ERR_UNSUPPORTED, "more than 2^31 tiles");
     static bool set[64] = {};

@@ -81,12 +81,12 @@ constexpr int kWgChunkSteps = 8;                 // 512 tokens
 // Tiles of 128 x 128, a cluster of `split` CTAs on each that take equal runs of tokens: their partial sums go to the CTA that
 // owns a group of four columns through distributed shared memory (the operand ring's, once every CTA of the cluster is
 // done with it), and are added in rank order.
-// Warps: 0 producer, 1 tensor memory and MMA issue, 2..9 workers: they transform every stage, and after a chunk's last one add up
-// the chunk before (warp w: lane quarter w % 4, half of the columns).
+// Warps: 0 producer of dy, 10 of codes and scales, 1 tensor memory and MMA issue, 2..9 workers: they transform the stages, and after a
+// chunk's last one add up the chunk before (warp w: lane quarter w % 4, half of the columns).
 
 constexpr int kWgBN = 128;
 constexpr int kWgWorkers = 8;
-constexpr int kWgThreads = 32 * (2 + kWgWorkers);
+constexpr int kWgThreads = 32 * (3 + kWgWorkers);
 constexpr int kWgOwn = kWgBN / 2;                                   // columns of a worker thread's row
 constexpr int kWgRaw = 2 * kWgBox;                                  // dy: two boxes
 constexpr int kWgCodes = kWgRaw, kWgScales = kWgCodes + kWgTokens * kWgBN, kWgX = kWgScales + kWgTokens * 16;
@@ -97,28 +97,35 @@ static_assert(kWgStages * kWgStage >= (128 + 8) * kWgBN * 4 && kWgStages <= kMax
 
 struct WgradSmall : MxCta {
     int64_t n0, k0;
+    __device__ uint32_t raw_bar(int s) const { return bars + (uint32_t)sizeof(MxBars) + (uint32_t)s * 8u; }
     int first, cols, groups, own, own_valid;
 
-    __device__ void produce(const CUtensorMap &map_dy, const CUtensorMap &map_codes, const CUtensorMap &map_scales, const WgradArgs &g) const
+    // Two producers: dy, on the full barriers; codes and scales, on the raw ones.  (One thread takes over 0.4 us to issue all
+    // four copies of a step.)
+    template <bool DY>
+    __device__ void produce(const CUtensorMap &map_a, const CUtensorMap &map_b, const WgradArgs &g) const
     {
         if (lane == 0) {
-            dep_launch();
+            if (DY) dep_launch();
             int it = 0, s = 0;
             uint32_t ph = 1;
             for (; it < steps; ++it) {
                 if (it >= S && !mbar_wait(empty_bar(s), ph, abort_flag, g.status, g.wait_limit)) break;
-                const uint32_t full = full_bar(s), at = smem + (uint32_t)(s * kWgStage);
+                const uint32_t bar = DY ? full_bar(s) : raw_bar(s), at = smem + (uint32_t)(s * kWgStage);
                 const int m = (first + it) * kWgTokens;
-                mbar_expect_tx(full, kWgX);
-                tma_load_2d(at, &map_dy, full, (int)n0, m);
-                tma_load_2d(at + kWgBox, &map_dy, full, (int)n0 + 64, m);
-                tma_load_2d(at + kWgCodes, &map_codes, full, (int)k0, m);
-                tma_load_2d(at + kWgScales, &map_scales, full, (int)(k0 / 32) & ~15, m);
+                mbar_expect_tx(bar, DY ? kWgCodes : kWgX - kWgCodes);
+                if (DY) {
+                    tma_load_2d(at, &map_a, bar, (int)n0, m);
+                    tma_load_2d(at + kWgBox, &map_a, bar, (int)n0 + 64, m);
+                } else {
+                    tma_load_2d(at + kWgCodes, &map_a, bar, (int)k0, m);
+                    tma_load_2d(at + kWgScales, &map_b, bar, (int)(k0 / 32) & ~15, m);
+                }
                 if (++s == S) { s = 0; ph ^= 1u; }
             }
             if (*abort_flag)       // none of this thread's copies may land after the CTA has exited
                 for (int j = it > S ? it - S : 0; j < it; ++j)
-                    mbar_wait(full_bar(j % S), (uint32_t)(j / S) & 1u, abort_flag, g.status, g.wait_limit, true);
+                    mbar_wait(DY ? full_bar(j % S) : raw_bar(j % S), (uint32_t)(j / S) & 1u, abort_flag, g.status, g.wait_limit, true);
         }
         __syncwarp();
     }
@@ -175,21 +182,24 @@ struct WgradSmall : MxCta {
 
     __device__ void work(const WgradArgs &g, float (&sum)[kWgOwn]) const
     {
-        const int wt = threadIdx.x - 64, chunk = wt & 15, t0 = wt >> 4;       // eight codes of every sixteenth token
+        // a team of four warps takes every other stage: one's barriers and loads run beside the other's arithmetic
+        const int team = (warp - 2) >> 2, wt = (threadIdx.x - 64) & 127, chunk = wt & 15, t0 = wt >> 4;    // eight codes of every eighth token
         const uint32_t src = kWgCodes + (uint32_t)(t0 * kWgBN + chunk * 8);
         const uint32_t sc = kWgScales + (uint32_t)(t0 * 16 + ((int)(k0 / 32) & 15) + (chunk >> 2));
-        const uint32_t dst = kWgX + (uint32_t)((chunk >> 3) * kWgBox + t0 * 128 + (((chunk & 7) ^ (t0 & 7)) << 4));
+        const uint32_t dst = kWgX + (uint32_t)((chunk >> 3) * kWgBox + t0 * 128 + (((chunk & 7) ^ t0) << 4));
 #pragma unroll
         for (int j = 0; j < kWgOwn; ++j) sum[j] = 0.0f;
         int s = 0, c = 0;
         uint32_t ph = 0;
         for (int it = 0; it < steps; ++it) {
-            mbar_wait(full_bar(s), ph, abort_flag, g.status, g.wait_limit);
-            const uint32_t at = smem + (uint32_t)(s * kWgStage);
-            transform_codes<kWgTokens / 16, 16>(at + src, at + sc, at + dst);
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(xf_bar(s));
+            if ((it & 1) == team) {
+                mbar_wait(raw_bar(s), ph, abort_flag, g.status, g.wait_limit);
+                const uint32_t at = smem + (uint32_t)(s * kWgStage);
+                transform_codes<kWgTokens / 8, 8>(at + src, at + sc, at + dst);
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(xf_bar(s));
+            }
             if (++s == S) { s = 0; ph ^= 1u; }
             if ((it & (kWgChunkSteps - 1)) == kWgChunkSteps - 1 && it < steps - 1) {
                 if (c > 0) add_chunk(g, c - 1, sum);
@@ -257,7 +267,7 @@ sparq_wgrad_small_kernel(const __grid_constant__ CUtensorMap map_dy, const __gri
                          const __grid_constant__ CUtensorMap map_scales, const WgradArgs g)
 {
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) MxBars bars;
+    __shared__ __align__(8) struct { MxBars bars; uint64_t raw[kMaxStages]; } room;
     __shared__ uint32_t tmem_base_slot;
     __shared__ uint32_t abort_word;
 
@@ -266,7 +276,7 @@ sparq_wgrad_small_kernel(const __grid_constant__ CUtensorMap map_dy, const __gri
     c.abort_flag = &abort_word;
     c.S = g.stages;
     c.smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    c.bars = smem_u32(&bars);
+    c.bars = smem_u32(&room);
     const uint32_t split = c.split = (uint32_t)g.split, tile = blockIdx.x / split;
     c.rank = (int)(blockIdx.x - tile * split);
     const uint32_t k_tiles = (uint32_t)((g.K + kWgBN - 1) / kWgBN), nt = tile / k_tiles;
@@ -287,7 +297,8 @@ sparq_wgrad_small_kernel(const __grid_constant__ CUtensorMap map_dy, const __gri
             prefetch_tensormap(&map_scales);
             for (int s = 0; s < c.S; ++s) {
                 mbar_init(c.full_bar(s), 1);
-                mbar_init(c.xf_bar(s), kWgWorkers);
+                mbar_init(c.raw_bar(s), 1);
+                mbar_init(c.xf_bar(s), 4);
                 mbar_init(c.empty_bar(s), 1);
             }
             for (int b = 0; b < 2; ++b) {
@@ -311,8 +322,9 @@ sparq_wgrad_small_kernel(const __grid_constant__ CUtensorMap map_dy, const __gri
     float sum[kWgOwn];
     dep_wait();
     switch (warp) {
-    case 0: c.produce(map_dy, map_codes, map_scales, g); break;
+    case 0: c.produce<true>(map_dy, map_dy, g); break;
     case 1: c.issue(g); break;
+    case 2 + kWgWorkers: c.produce<false>(map_codes, map_scales, g); break;
     default: c.work(g, sum);
     }
     // Every MMA of this CTA has retired (or a wait gave up), and none of its copies is on its way: the cluster's rings are
@@ -322,7 +334,7 @@ sparq_wgrad_small_kernel(const __grid_constant__ CUtensorMap map_dy, const __gri
         cluster_arrive();
         cluster_wait();
     }
-    if (warp >= 2) c.finish(g, sum);
+    if (warp >= 2 && warp < 2 + kWgWorkers) c.finish(g, sum);
     __syncthreads();
     // No CTA leaves while its peers' rows are on their way to it: every CTA sends all of its rows, after a wait that gave up
     // too, and finish() waits for them whether or not the flag is up.
