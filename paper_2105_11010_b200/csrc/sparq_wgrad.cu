@@ -19,6 +19,36 @@ cudaError_t launch_wgrad(Kernel kernel, bool (&attr_set)[64], int grid, int clus
     return e == cudaSuccess ? launch_overlapped_cluster(kernel, grid, cluster, threads, smem, st, dy, codes, scales, args) : e;
 }
 
+struct WgradForm {
+    bool pairs, expand;     // pairs of CTAs on 256 x 256 tiles, X expanded to bf16 first
+    int split, parts;
+    int64_t tiles;
+};
+
+// By estimates of the time in us.
+WgradForm pick_wgrad(int64_t M, int64_t N, int64_t K, int blocks, int sms)
+{
+    WgradForm best = {};
+    double cost = 1e30;
+    const int64_t small = (N + 127) / 128 * ((K + 127) / 128), large = (N + 255) / 256 * ((K + 255) / 256);
+    const double expand = 3.0 + (double)M * (double)K * 3.0 / 6.0e6;
+    for (int parts = 1; parts <= 128 && parts * 8 <= blocks + 7; parts += parts < 8 ? 1 : parts < 32 ? 4 : 16) {
+        const int b = (blocks + parts - 1) / parts;
+        const double join = parts > 1 ? 3.0 + (double)(parts + 1) * (double)N * (double)K * 4.0 / 5.0e6 : 0.0;
+        if (parts > 1 && (double)parts * (double)N * (double)K * 4.0 > (double)kWorkspaceMaxBytes) break;
+        for (int split = 1; split <= 8 && split <= b; split *= 2) {
+            const int64_t at_once = clusters_at_once(split, sms), rounds = (small * parts + at_once - 1) / at_once;
+            const double c = join + 0.5 + (double)rounds * (4.2 + 0.45 * ((b + split - 1) / split) + (split > 1 ? 1.5 : 0.0));
+            if (c < cost - 0.05) { cost = c; best = {false, false, split, parts, small}; }
+        }
+        const int64_t rounds = (large * parts + sms / 2 - 1) / (sms / 2);
+        const double q = join + 4.5 + (double)rounds * 0.5 * b, x = join + 4.5 + expand + (double)rounds * 0.36 * b;
+        if (q < cost - 0.05) { cost = q; best = {true, false, 1, parts, large}; }
+        if (x < cost - 0.05 && (double)M * (double)mx_padded(K) * 2.0 <= (double)kWorkspaceMaxBytes) { cost = x; best = {true, true, 1, parts, large}; }
+    }
+    return best;
+}
+
 }  // namespace
 
 }  // namespace sparq
@@ -61,39 +91,53 @@ extern "C" int sparq_wgrad_mx8(const void *dy, int64_t lddy, const int8_t *codes
     CUtensorMap map_dy, map_codes, map_scales;
     const int64_t pitch = mx_code_pitch(SPARQ_MXINT8, K), spitch = mx_scale_cols(SPARQ_MXINT8, K);
     if ((rc = encode_matrix(&map_dy, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, dy, N, M, lddy * 2, 64, kWgTokens, CU_TENSOR_MAP_SWIZZLE_128B)) != SPARQ_OK) return rc;
-    if ((rc = encode_matrix(&map_codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, pitch, M, pitch, kWgBN, kWgTokens, CU_TENSOR_MAP_SWIZZLE_NONE)) != SPARQ_OK) return rc;
+    if ((rc = encode_matrix(&map_codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, pitch, M, pitch, kWgBN, kWgTokens, CU_TENSOR_MAP_SWIZZLE_128B)) != SPARQ_OK) return rc;
     if ((rc = encode_matrix(&map_scales, CU_TENSOR_MAP_DATA_TYPE_UINT8, scales, spitch, M, spitch, 16, kWgTokens, CU_TENSOR_MAP_SWIZZLE_NONE)) != SPARQ_OK) return rc;
-    const int64_t n_tiles = (N + kWgTile - 1) / kWgTile, k_tiles = (K + kWgTile - 1) / kWgTile;
-    if (n_tiles * k_tiles >= 16 && n_tiles * k_tiles <= INT64_C(1) << 30) {
-        const int pairs = (int)(n_tiles * k_tiles < sms / 2 ? n_tiles * k_tiles : sms / 2);
-        const WgradPairArgs p = {g, (int)n_tiles, (int)k_tiles, pairs};
-        // expanded first, into scratch memory
-        const size_t x_bytes = (size_t)M * (size_t)pitch * 2;
-        if (n_tiles >= 3) {
-            if (void *x = workspace_alloc(x_bytes, st)) {
-                CUtensorMap map_x;
-                rc = sparq_dequantize_mx(codes, scales, M, K, SPARQ_MXINT8, nullptr, x, SPARQ_DTYPE_BF16, pitch, stream);
-                if (rc == SPARQ_OK)
-                    rc = encode_matrix(&map_x, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, x, K, M, pitch * 2, 64, kWgTokens, CU_TENSOR_MAP_SWIZZLE_128B);
-                if (rc == SPARQ_OK) {
-                    static bool set[64] = {};
-                    const cudaError_t ce = launch_wgrad(sparq_wgrad_kernel<true>, set, 2 * pairs, 2, kWgPairThreads, wgrad_smem(true), st, map_dy, map_x, map_x, p);
-                    if (ce != cudaSuccess) rc = cuda_error(ce, "sparq_wgrad_kernel launch");
-                }
-                workspace_free(x, st);
-                return rc;
-            }
-        }
-        static bool set[64] = {};
-        const cudaError_t ce = launch_wgrad(sparq_wgrad_kernel<false>, set, 2 * pairs, 2, kWgPairThreads, wgrad_smem(false), st, map_dy, map_codes, map_scales, p);
-        return ce == cudaSuccess ? SPARQ_OK : cuda_error(ce, "sparq_wgrad_kernel launch");
+    const WgradForm form = pick_wgrad(M, N, K, g.blocks, sms);
+    g.parts = form.parts;
+    g.split = form.split;
+    if (form.tiles * form.parts * form.split > INT64_C(1) << 30) return set_error(SPARQ_ERR_UNSUPPORTED, "more than 2^30 tiles");
+    // Scratch memory for X in bf16 and for the parts' sums.  Without it (a stream that is being captured) X is expanded stage by stage and
+    // the parts add to dw one launch after the other: the same sums in the same order.
+    CUtensorMap map_x;
+    void *x = form.expand ? workspace_alloc((size_t)M * (size_t)pitch * 2, st) : nullptr;
+    float *sums = form.parts > 1 ? (float *)workspace_alloc((size_t)form.parts * (size_t)N * (size_t)K * sizeof(float), st) : nullptr;
+    rc = SPARQ_OK;
+    if (x) {
+        rc = sparq_dequantize_mx(codes, scales, M, K, SPARQ_MXINT8, nullptr, x, SPARQ_DTYPE_BF16, pitch, stream);
+        if (rc == SPARQ_OK) rc = encode_matrix(&map_x, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, x, K, M, pitch * 2, 64, kWgTokens, CU_TENSOR_MAP_SWIZZLE_128B);
     }
-    const int64_t tiles = (N + 127) / 128 * ((K + kWgBN - 1) / kWgBN);
-    g.split = 1;
-    while (g.split < 8 && tiles <= clusters_at_once(2 * g.split, sms) && g.blocks >= 2 * g.split) g.split *= 2;
-    g.stages = kWgStages;
-    if (tiles * g.split > INT64_C(2147483647)) return set_error(SPARQ_ERR_UNSUPPORTED, "more than 2^31 tiles");
-    static bool set[64] = {};
-    const cudaError_t e = launch_wgrad(sparq_wgrad_small_kernel, set, (int)(tiles * g.split), g.split, kWgThreads, wgrad_smem(false), st, map_dy, map_codes, map_scales, g);
-    return e == cudaSuccess ? SPARQ_OK : cuda_error(e, "sparq_wgrad_small_kernel launch");
+    const int launches = sums ? 1 : g.parts;
+    if (sums) {
+        g.dw = sums;
+        g.part_stride = N * K;
+        g.accumulate = 0;
+    }
+    g.count = sums ? g.parts : 1;
+    for (int l = 0; l < launches && rc == SPARQ_OK; ++l) {
+        g.part = l;
+        if (!sums) g.accumulate = accumulate != 0 || l > 0;
+        cudaError_t e;
+        if (form.pairs) {
+            const int64_t items = form.tiles * g.count;
+            const WgradPairArgs p = {g, (int)((N + kWgTile - 1) / kWgTile), (int)((K + kWgTile - 1) / kWgTile), (int)(items < sms / 2 ? items : sms / 2)};
+            static bool set_x[64] = {}, set_q[64] = {};
+            e = x ? launch_wgrad(sparq_wgrad_kernel<true>, set_x, 2 * p.pairs, 2, kWgPairThreads, wgrad_smem(true), st, map_dy, map_x, map_x, p)
+                  : launch_wgrad(sparq_wgrad_kernel<false>, set_q, 2 * p.pairs, 2, kWgPairThreads, wgrad_smem(false), st, map_dy, map_codes, map_scales, p);
+        } else {
+            static bool set[64] = {};
+            e = launch_wgrad(sparq_wgrad_small_kernel, set, (int)(form.tiles * g.count * g.split), g.split, kWgThreads, wgrad_smem(false), st,
+                             map_dy, map_codes, map_scales, g);
+        }
+        if (e != cudaSuccess) rc = cuda_error(e, "weight gradient kernel launch");
+    }
+    if (sums && rc == SPARQ_OK) {
+        const int64_t threads = (N * K + 3) / 4, blocks = (threads + 255) / 256;
+        const cudaError_t e = launch_overlapped(wgrad_add_parts_kernel, (int)(blocks < 8 * sms ? blocks : 8 * sms), 256, 0, st, (const float *)sums, N * K,
+                                                g.parts, (int)(accumulate != 0), dw);
+        if (e != cudaSuccess) rc = cuda_error(e, "wgrad_add_parts_kernel launch");
+    }
+    workspace_free(sums, st);
+    workspace_free(x, st);
+    return rc;
 }

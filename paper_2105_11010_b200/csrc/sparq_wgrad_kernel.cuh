@@ -13,14 +13,19 @@
 
 namespace sparq {
 
+// The tokens are cut into `parts` equal runs of steps whose sums are added in order.  A launch takes `count` of them from `part` on and
+// writes each one's sums `part_stride` elements after the one's before: all parts into scratch memory that another launch adds up,
+// or one part after the other into dw itself.
 struct WgradArgs {
     int64_t M, N, K;
     int blocks;                 // reduction steps of kWgTokens
+    int parts, part, count;
+    int64_t part_stride;
     int accumulate;
     float *dw;
     unsigned int *status;
     long long wait_limit;
-    int stages, split;
+    int split;
 };
 
 constexpr int kWgTokens = 64;                    // per reduction step: four MMAs of 16
@@ -35,10 +40,11 @@ __device__ __forceinline__ uint32_t bf16_scale_pair(uint32_t code)
     return prmt(b, b, 0x1010u);
 }
 
-// Four codes of one block as bf16 values.  As bit patterns in bf16, whose steps are 1 in [128, 256) and 2 in [256, 512):
+// Four codes of one block as bf16 values, in the order 0, 2, 1, 3: the columns of the operand and so of the accumulator, which are put in
+// order when they are written out.  As bit patterns in bf16, whose steps are 1 in [128, 256) and 2 in [256, 512):
 //     0x4300 | (b & 0x7F) = 128 + (b & 0x7F),   0x4300 | (b & 0x80) = 128 or 256,
 // and their difference is the two's complement value; difference and product with a power of two are exact.
-__device__ __forceinline__ void codes_to_bf16(uint32_t w, uint32_t scale, uint32_t &lo, uint32_t &hi)
+__device__ __forceinline__ void codes_to_bf16(uint32_t w, uint32_t scale, uint32_t &even, uint32_t &odd)
 {
     auto two = [&](uint32_t p) {
         const uint32_t v = (p & 0x007F007Fu) | 0x43004300u, c = (p & 0x00800080u) | 0x43004300u;
@@ -46,28 +52,42 @@ __device__ __forceinline__ void codes_to_bf16(uint32_t w, uint32_t scale, uint32
         asm("{\n\t.reg .b32 t;\n\tsub.rn.bf16x2 t, %1, %2;\n\tmul.rn.bf16x2 %0, t, %3;\n\t}" : "=r"(d) : "r"(v), "r"(c), "r"(scale));
         return d;
     };
-    lo = two(prmt(w, 0u, 0x4140u));
-    hi = two(prmt(w, 0u, 0x4342u));
+    even = two(w);
+    odd = two(w >> 8);
 }
+__host__ __device__ constexpr int wgrad_column(int j) { return (j & ~3) | ((j & 1) << 1) | ((j >> 1) & 1); }
 
-// ITEMS times eight codes of a thread -- of tokens `STEP` apart, in a raw tile with rows of 128 codes and of 16 scales -- into an
-// operand tile.  All loads go out before the first store: one item after the other took a stage 1.2 us, chains of latency.
-template <int ITEMS, int STEP>
-__device__ __forceinline__ void transform_codes(uint32_t src, uint32_t sc, uint32_t dst)
+// A team of 128 threads turns a raw tile (64 tokens x 128 codes, swizzled by TMA; rows of 16 scales) into an operand tile (two atoms of 64
+// columns).  A thread takes 16 codes of every sixteenth token.  Eight neighbouring lanes take half a row each of tokens t and t ^ 5, whose
+// swizzles differ in bits 0 and 2: loads and stores of 16 bytes then meet all banks.  All loads go out before the first store.
+struct TeamPlace {
+    uint32_t src, sc, dst0, dst1;           // offsets in a stage
+    __device__ TeamPlace(int thread, int scale_offset, uint32_t codes_at, uint32_t scales_at, uint32_t x_at)
+    {
+        const int c4 = thread & 3, atom = (thread >> 3) & 1, u = thread >> 4;
+        const int t = ((u & 3) | ((u & 4) << 1)) ^ (thread & 4 ? 5 : 0), x = t & 7;
+        src = codes_at + (uint32_t)(t * 128 + (((atom * 4 + c4) ^ x) << 4));
+        sc = scales_at + (uint32_t)(t * 16 + scale_offset + atom * 2 + (c4 >> 1));
+        dst0 = x_at + (uint32_t)(atom * (64 * 128) + t * 128 + (((2 * c4) ^ x) << 4));
+        dst1 = x_at + (uint32_t)(atom * (64 * 128) + t * 128 + (((2 * c4 + 1) ^ x) << 4));
+    }
+};
+__device__ __forceinline__ void transform_stage(uint32_t at, const TeamPlace &p)
 {
-    uint32_t a[ITEMS], b[ITEMS], code[ITEMS];
+    uint32_t w[4][4], code[4];
 #pragma unroll
-    for (int j = 0; j < ITEMS; ++j) {
-        asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(a[j]), "=r"(b[j]) : "r"(src + (uint32_t)(j * STEP * 128)));
-        asm volatile("ld.shared.u8 %0, [%1];" : "=r"(code[j]) : "r"(sc + (uint32_t)(j * STEP * 16)));
+    for (int j = 0; j < 4; ++j) {
+        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[j][0]), "=r"(w[j][1]), "=r"(w[j][2]), "=r"(w[j][3]) : "r"(at + p.src + (uint32_t)(j * 16 * 128)));
+        asm volatile("ld.shared.u8 %0, [%1];" : "=r"(code[j]) : "r"(at + p.sc + (uint32_t)(j * 16 * 16)));
     }
 #pragma unroll
-    for (int j = 0; j < ITEMS; ++j) {
+    for (int j = 0; j < 4; ++j) {
         const uint32_t scale = bf16_scale_pair(code[j]);
-        uint32_t x0, x1, x2, x3;
-        codes_to_bf16(a[j], scale, x0, x1);
-        codes_to_bf16(b[j], scale, x2, x3);
-        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" :: "r"(dst + (uint32_t)(j * STEP * 128)), "r"(x0), "r"(x1), "r"(x2), "r"(x3) : "memory");
+        uint32_t x[8];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) codes_to_bf16(w[j][q], scale, x[2 * q], x[2 * q + 1]);
+        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" :: "r"(at + p.dst0 + (uint32_t)(j * 16 * 128)), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
+        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" :: "r"(at + p.dst1 + (uint32_t)(j * 16 * 128)), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]) : "memory");
     }
 }
 
@@ -97,6 +117,7 @@ static_assert(kWgStages * kWgStage >= (128 + 8) * kWgBN * 4 && kWgStages <= kMax
 
 struct WgradSmall : MxCta {
     int64_t n0, k0;
+    float *dw;
     __device__ uint32_t raw_bar(int s) const { return bars + (uint32_t)sizeof(MxBars) + (uint32_t)s * 8u; }
     int first, cols, groups, own, own_valid;
 
@@ -183,10 +204,8 @@ struct WgradSmall : MxCta {
     __device__ void work(const WgradArgs &g, float (&sum)[kWgOwn]) const
     {
         // a team of four warps takes every other stage: one's barriers and loads run beside the other's arithmetic
-        const int team = (warp - 2) >> 2, wt = (threadIdx.x - 64) & 127, chunk = wt & 15, t0 = wt >> 4;    // eight codes of every eighth token
-        const uint32_t src = kWgCodes + (uint32_t)(t0 * kWgBN + chunk * 8);
-        const uint32_t sc = kWgScales + (uint32_t)(t0 * 16 + ((int)(k0 / 32) & 15) + (chunk >> 2));
-        const uint32_t dst = kWgX + (uint32_t)((chunk >> 3) * kWgBox + t0 * 128 + (((chunk & 7) ^ t0) << 4));
+        const int team = (warp - 2) >> 2;
+        const TeamPlace place((threadIdx.x - 64) & 127, (int)(k0 / 32) & 15, kWgCodes, kWgScales, kWgX);
 #pragma unroll
         for (int j = 0; j < kWgOwn; ++j) sum[j] = 0.0f;
         int s = 0, c = 0;
@@ -194,8 +213,7 @@ struct WgradSmall : MxCta {
         for (int it = 0; it < steps; ++it) {
             if ((it & 1) == team) {
                 mbar_wait(raw_bar(s), ph, abort_flag, g.status, g.wait_limit);
-                const uint32_t at = smem + (uint32_t)(s * kWgStage);
-                transform_codes<kWgTokens / 8, 8>(at + src, at + sc, at + dst);
+                transform_stage(smem + (uint32_t)(s * kWgStage), place);
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(xf_bar(s));
@@ -216,7 +234,7 @@ struct WgradSmall : MxCta {
         const int64_t n = n0 + quarter * 32 + lane;
         auto put = [&](int col, const float (&a)[4]) {
             if (n >= g.N) return;
-            float *out = g.dw + n * g.K + k0 + col;
+            float *out = dw + n * g.K + k0 + col;
             if (col + 4 <= cols && (reinterpret_cast<uintptr_t>(out) & 15u) == 0) {
                 float4 v = make_float4(a[0], a[1], a[2], a[3]);
                 if (g.accumulate) {
@@ -234,7 +252,7 @@ struct WgradSmall : MxCta {
         for (int q = 0; q < kWgOwn / 4; ++q) {
             const int grp = half * (kWgOwn / 4) + q;
             if (grp >= groups) continue;
-            const float a[4] = {sum[4 * q], sum[4 * q + 1], sum[4 * q + 2], sum[4 * q + 3]};
+            const float a[4] = {sum[4 * q], sum[4 * q + wgrad_column(1)], sum[4 * q + wgrad_column(2)], sum[4 * q + 3]};
             if (split == 1) {
                 put(grp * 4, a);
             } else {
@@ -274,16 +292,21 @@ sparq_wgrad_small_kernel(const __grid_constant__ CUtensorMap map_dy, const __gri
     WgradSmall c;
     const int warp = c.warp = threadIdx.x >> 5, lane = c.lane = threadIdx.x & 31;
     c.abort_flag = &abort_word;
-    c.S = g.stages;
+    c.S = kWgStages;
     c.smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
     c.bars = smem_u32(&room);
-    const uint32_t split = c.split = (uint32_t)g.split, tile = blockIdx.x / split;
-    c.rank = (int)(blockIdx.x - tile * split);
-    const uint32_t k_tiles = (uint32_t)((g.K + kWgBN - 1) / kWgBN), nt = tile / k_tiles;
+    const uint32_t split = c.split = (uint32_t)g.split, item = blockIdx.x / split;
+    c.rank = (int)(blockIdx.x - item * split);
+    const uint32_t k_tiles = (uint32_t)((g.K + kWgBN - 1) / kWgBN), tiles = k_tiles * (uint32_t)((g.N + 127) / 128);
+    const uint32_t in = item / tiles, tile = item - in * tiles, nt = tile / k_tiles;
     c.n0 = (int64_t)nt * 128;
     c.k0 = (int64_t)(tile - nt * k_tiles) * kWgBN;
-    c.first = (int)((int64_t)c.rank * g.blocks / split);
-    c.steps = (int)((int64_t)(c.rank + 1) * g.blocks / split) - c.first;
+    c.dw = g.dw + in * g.part_stride;
+    // this part's steps, and this CTA's of them
+    const int part = g.part + (int)in, part_first = (int)((int64_t)part * g.blocks / g.parts);
+    const int part_steps = (int)((int64_t)(part + 1) * g.blocks / g.parts) - part_first;
+    c.first = part_first + (int)((int64_t)c.rank * part_steps / split);
+    c.steps = part_first + (int)((int64_t)(c.rank + 1) * part_steps / split) - c.first;
     c.cols = g.K - c.k0 < kWgBN ? (int)(g.K - c.k0) : kWgBN;
     c.groups = (c.cols + 3) / 4;
     c.own = (c.groups + (int)split - 1) / (int)split;
@@ -368,9 +391,16 @@ struct WgradPairArgs {
     int n_tiles, k_tiles, pairs;
 };
 
-// Tile t in an order that keeps eight rows of tiles together.
-__device__ __forceinline__ void wgrad_tile(const WgradPairArgs &p, int t, int &nt, int &kt)
+// Steps of part p.
+__device__ __forceinline__ int part_begin(const WgradArgs &g, int p) { return (int)((int64_t)p * g.blocks / g.parts); }
+
+// Item t: its part, and its tile in an order that keeps eight rows of tiles together.
+__device__ __forceinline__ void wgrad_tile(const WgradPairArgs &p, int t, int &part, int &nt, int &kt)
 {
+    const int tiles = p.n_tiles * p.k_tiles;
+    part = t / tiles;
+    t -= part * tiles;
+    part += p.g.part;
     const int per_group = 8 * p.k_tiles, group = t / per_group, first = group * 8;
     const int rows = p.n_tiles - first < 8 ? p.n_tiles - first : 8, in = t - group * per_group;
     kt = in / rows;
@@ -396,10 +426,10 @@ struct WgradPair : MxCta {
             uint32_t ph = 1;
             bool live = true;
             for (int t = pair; t < tiles && live; t += p.pairs) {
-                int nt, kt;
-                wgrad_tile(p, t, nt, kt);
+                int part, nt, kt;
+                wgrad_tile(p, t, part, nt, kt);
                 const int n = nt * kWgTile + rank * 128, k = kt * kWgTile + rank * 128, sc = (k / 32) & ~15;
-                for (int b = 0; b < g.blocks; ++b) {
+                for (int b = part_begin(g, part), last = part_begin(g, part + 1); b < last; ++b) {
                     if (used >= kStages && !mbar_wait(empty_bar(s), ph, abort_flag, g.status, g.wait_limit)) { live = false; break; }
                     const uint32_t at = smem + (uint32_t)(s * kStage);
                     const int m = b * kWgTokens;
@@ -445,13 +475,14 @@ struct WgradPair : MxCta {
             int s = 0, c = 0;
             uint32_t ph = 0;
             for (int t = pair; t < tiles; t += p.pairs) {
-                for (int b = 0; b < g.blocks; ++b) {
+                const int part = g.part + t / (p.n_tiles * p.k_tiles), steps_of = part_begin(g, part + 1) - part_begin(g, part);
+                for (int b = 0; b < steps_of; ++b) {
                     const int in = b & (kWgChunkSteps - 1);
                     if (in == 0 && c >= 2) mbar_wait(freed_bar(c & 1), (uint32_t)((c >> 1) - 1) & 1u, abort_flag, g.status, g.wait_limit);
                     mbar_wait(full_bar(s), ph, abort_flag, g.status, g.wait_limit);
                     if (!X16) mbar_wait(xf_bar(s), ph, abort_flag, g.status, g.wait_limit);
                     tc_fence_after();
-                    const bool chunk_ends = in == kWgChunkSteps - 1 || b == g.blocks - 1;
+                    const bool chunk_ends = in == kWgChunkSteps - 1 || b == steps_of - 1;
                     if (elected) {
                         const uint32_t at = smem + (uint32_t)(s * kStage), d = tmem + (uint32_t)((c & 1) * kWgTile);
                         const uint64_t adesc = mn_major_desc(at, kWgBox), bdesc = mn_major_desc(at + kXAt, kWgBox);
@@ -490,10 +521,11 @@ struct WgradPair : MxCta {
         if (lane == 0) mbar_arrive_remote(leader_freed + 8u * (uint32_t)(c & 1));
     }
 
-    __device__ void write(const WgradArgs &g, int64_t n, int64_t k, const float (&sum)[kWgPairOwn]) const
+    __device__ void write(const WgradArgs &g, float *dw, int64_t n, int64_t k, const float (&sum)[kWgPairOwn]) const
     {
         if (n >= g.N) return;
-        float *out = g.dw + n * g.K + k;
+        float *out = dw + n * g.K + k;
+        auto at = [](int j) { return X16 ? j : wgrad_column(j); };       // of column j in the accumulator
         if (k + kWgPairOwn <= g.K && (reinterpret_cast<uintptr_t>(out) & 31u) == 0) {
 #pragma unroll
             for (int j = 0; j < kWgPairOwn; j += 8) {
@@ -501,10 +533,10 @@ struct WgradPair : MxCta {
                 if (g.accumulate) {
                     ld_v8(v, out + j);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] = __float_as_uint(__fadd_rn(__uint_as_float(v[i]), sum[j + i]));
+                    for (int i = 0; i < 8; ++i) v[i] = __float_as_uint(__fadd_rn(__uint_as_float(v[i]), sum[at(j + i)]));
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] = __float_as_uint(sum[j + i]);
+                    for (int i = 0; i < 8; ++i) v[i] = __float_as_uint(sum[at(j + i)]);
                 }
                 st_v8(out + j, v);
             }
@@ -512,39 +544,36 @@ struct WgradPair : MxCta {
         }
 #pragma unroll
         for (int j = 0; j < kWgPairOwn; ++j)
-            if (k + j < g.K) out[j] = g.accumulate ? __fadd_rn(out[j], sum[j]) : sum[j];
+            if (k + j < g.K) out[j] = g.accumulate ? __fadd_rn(out[j], sum[at(j)]) : sum[at(j)];
     }
 
     __device__ void work(const WgradPairArgs &p) const
     {
         const WgradArgs &g = p.g;
         // a team of four warps takes every other stage: one's barriers and loads run beside the other's arithmetic
-        const int team = (warp - kWgFirstWorker) >> 2, wt = threadIdx.x & 127, chunk = wt & 15, t0 = wt >> 4;    // eight codes of every eighth token
-        const uint32_t src = kWgCodes + (uint32_t)(t0 * kWgBN + chunk * 8);
-        const uint32_t dst = kWgX + (uint32_t)((chunk >> 3) * kWgBox + t0 * 128 + (((chunk & 7) ^ t0) << 4));
+        const int team = (warp - kWgFirstWorker) >> 2;
         const uint32_t leader_xf = map_to_rank(xf_bar(0), 0), leader_freed = map_to_rank(freed_bar(0), 0);
         int s = 0, c = 0, stage = 0;
         uint32_t ph = 0;
         for (int t = pair; t < tiles; t += p.pairs) {
-            int nt, kt;
-            wgrad_tile(p, t, nt, kt);
-            const int k0 = kt * kWgTile + rank * 128;
-            const uint32_t sc = kWgScales + (uint32_t)(t0 * 16 + ((k0 / 32) & 15) + (chunk >> 2));
+            int part, nt, kt;
+            wgrad_tile(p, t, part, nt, kt);
+            const int steps_of = part_begin(g, part + 1) - part_begin(g, part);
+            const TeamPlace place(threadIdx.x & 127, ((kt * kWgTile + rank * 128) / 32) & 15, kWgCodes, kWgScales, kWgX);
             float sum[kWgPairOwn];
 #pragma unroll
             for (int j = 0; j < kWgPairOwn; ++j) sum[j] = 0.0f;
             const int c_first = c;
-            for (int b = 0; b < g.blocks; ++b) {
+            for (int b = 0; b < steps_of; ++b) {
                 if (!X16 && (stage++ & 1) == team) {
                     mbar_wait(raw_bar(s), ph, abort_flag, g.status, g.wait_limit);
-                    const uint32_t at = smem + (uint32_t)(s * kStage);
-                    transform_codes<kWgTokens / 8, 8>(at + src, at + sc, at + dst);
+                    transform_stage(smem + (uint32_t)(s * kStage), place);
                     fence_proxy_async_smem();
                     __syncwarp();
                     if (lane == 0) mbar_arrive_remote(leader_xf + 8u * (uint32_t)s);
                 }
                 if (!X16 && ++s == kStages) { s = 0; ph ^= 1u; }
-                if ((b & (kWgChunkSteps - 1)) == kWgChunkSteps - 1 && b < g.blocks - 1) {
+                if ((b & (kWgChunkSteps - 1)) == kWgChunkSteps - 1 && b < steps_of - 1) {
                     if (c > c_first) add_chunk(g, c - 1, leader_freed, sum);
                     ++c;
                 }
@@ -552,7 +581,7 @@ struct WgradPair : MxCta {
             if (c > c_first) add_chunk(g, c - 1, leader_freed, sum);
             add_chunk(g, c, leader_freed, sum);
             ++c;
-            write(g, (int64_t)nt * kWgTile + rank * 128 + (warp & 3) * 32 + lane, (int64_t)kt * kWgTile + ((warp - kWgFirstWorker) >> 2) * kWgPairOwn, sum);
+            write(g, g.dw + (part - g.part) * g.part_stride, (int64_t)nt * kWgTile + rank * 128 + (warp & 3) * 32 + lane, (int64_t)kt * kWgTile + ((warp - kWgFirstWorker) >> 2) * kWgPairOwn, sum);
         }
     }
 };
@@ -575,7 +604,7 @@ sparq_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_cons
     c.bars = smem_u32(&room);
     c.rank = (int)(blockIdx.x & 1u);
     c.pair = (int)(blockIdx.x >> 1);
-    c.tiles = p.n_tiles * p.k_tiles;
+    c.tiles = p.n_tiles * p.k_tiles * p.g.count;
 
     if (warp == 0) {
         if (lane == 0) {
@@ -628,6 +657,31 @@ sparq_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_cons
     if (warp == 1) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" :: "r"(c.tmem), "r"(512u) : "memory");
+    }
+}
+
+// dw (+)= the parts' sums, one after the other.
+__global__ void __launch_bounds__(256)
+wgrad_add_parts_kernel(const float *sums, int64_t count, int parts, int accumulate, float *dw)
+{
+    const bool vec = (count & 3) == 0 && (reinterpret_cast<uintptr_t>(dw) & 15u) == 0;
+    const int64_t stride = (int64_t)gridDim.x * 256 * (vec ? 4 : 1);
+    dep_wait();
+    dep_launch();
+    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * (vec ? 4 : 1); i < count; i += stride) {
+        if (vec) {
+            float4 a = *reinterpret_cast<const float4 *>(accumulate ? dw + i : sums + i);
+#pragma unroll 4
+            for (int p = accumulate ? 0 : 1; p < parts; ++p) {
+                const float4 v = *reinterpret_cast<const float4 *>(sums + p * count + i);
+                a = make_float4(__fadd_rn(a.x, v.x), __fadd_rn(a.y, v.y), __fadd_rn(a.z, v.z), __fadd_rn(a.w, v.w));
+            }
+            *reinterpret_cast<float4 *>(dw + i) = a;
+        } else {
+            float a = accumulate ? dw[i] : sums[i];
+            for (int p = accumulate ? 0 : 1; p < parts; ++p) a = __fadd_rn(a, sums[p * count + i]);
+            dw[i] = a;
+        }
     }
 }
 
