@@ -388,10 +388,17 @@ SPARQ_API int sparq_act_backward_mx8(const void *dy, int dtype, int64_t rows, in
  *     dw[j][k] = sum_m dy[m][j] * X[m][k]   (+ dw[j][k] where accumulate is not 0)
  * dy is M x N bf16, row m at dy + m * lddy; dw is N x K fp32 with leading dimension K.  Products are
  * exact, sums are held in fp32 in an order that depends on the sizes only.  M == 0 leaves dw zero (as it is, accumulating).
- * Requirements (else SPARQ_ERR_UNSUPPORTED): dy 16-byte aligned, lddy a multiple of 8, dw aligned to its
- * elements, M, N and K below 2^31 - 256. */
+ * Requirements (else SPARQ_ERR_UNSUPPORTED): dy 16-byte aligned, lddy a multiple of 8 (any for M == 1), dw
+ * aligned to its elements, M, N and K below 2^31 - 256.
+ * workspace: DEVICE memory of sparq_wgrad_mx8_workspace_bytes, 256-byte aligned, the caller's until the work
+ * ends; or NULL, and the call takes scratch memory as the fused calls do.  While the stream is being captured
+ * there is no scratch memory, and a call without a workspace is slower, up to many times for a long sum into a small
+ * dw.  Same results, bit for bit.  Calls, and replays of graphs, that may overlap must not share a workspace. */
 SPARQ_API int sparq_wgrad_mx8(const void *dy, int64_t lddy, const int8_t *codes, const uint8_t *scales,
-                    int64_t M, int64_t N, int64_t K, int accumulate, float *dw, void *stream);
+                    int64_t M, int64_t N, int64_t K, int accumulate, float *dw,
+                    void *workspace, size_t workspace_bytes, void *stream);
+/* Bytes of workspace for these sizes on the current device (may be 0), or a negative sparq_status. */
+SPARQ_API int64_t sparq_wgrad_mx8_workspace_bytes(int64_t M, int64_t N, int64_t K);
 
 /* ---- 2:4 sparse weights (Sections 4 and 5.3) ---------------------------------------------
  * Weights pruned 2:4 arrive compressed as a sparse tensor core stores them: per output

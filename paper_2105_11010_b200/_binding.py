@@ -113,7 +113,8 @@ def load_library() -> ctypes.CDLL:
         L.sparq_gemm_mxf4.argtypes = [vp, vp, vp, vp, i64, i64, i64, i32, ctypes.POINTER(_CMxEpilogue), vp]
         L.sparq_act_forward_mx8.argtypes = [vp, vp, i32, i64, i64, i64, i32, vp, i64, vp, vp, vp, vp, vp]
         L.sparq_act_backward_mx8.argtypes = [vp, i32, i64, i64, i64, i32, vp, vp, vp, vp, vp, vp, i64, vp]
-        L.sparq_wgrad_mx8.argtypes = [vp, i64, vp, vp, i64, i64, i64, i32, vp, vp]
+        L.sparq_wgrad_mx8.argtypes = [vp, i64, vp, vp, i64, i64, i64, i32, vp, vp, sz, vp]
+        L.sparq_wgrad_mx8_workspace_bytes.argtypes, L.sparq_wgrad_mx8_workspace_bytes.restype = [i64, i64, i64], i64
         for f in (L.sparq_quantize_mx, L.sparq_dequantize_mx, L.sparq_gemm_mxf4, L.sparq_act_forward_mx8,
                   L.sparq_act_backward_mx8, L.sparq_wgrad_mx8):
             f.restype = i32
@@ -437,10 +438,21 @@ def sparq_act_backward_mx8(dy: torch.Tensor, codes: torch.Tensor, scales: torch.
         _raise(rc)
 
 
+def sparq_wgrad_mx8_workspace_bytes(M: int, N: int, K: int) -> int:
+    """Bytes of a workspace for :func:`sparq_wgrad_mx8` of these sizes on the current device."""
+    rc = load_library().sparq_wgrad_mx8_workspace_bytes(int(M), int(N), int(K))
+    if rc < 0:
+        _raise(int(rc))
+    return int(rc)
+
+
 def sparq_wgrad_mx8(dy: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, dw: torch.Tensor, *,
-                    accumulate: bool = False, stream=None) -> None:
-    """``dw (N, K) = dy^T @ X`` (``+ dw``) with ``dy`` (M, N) bfloat16 and X (M, K) kept as MXINT8."""
-    rc = _native.wgrad_mx8(dy, codes, scales, dw, accumulate, stream)
+                    accumulate: bool = False, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """``dw (N, K) = dy^T @ X`` (``+ dw``) with ``dy`` (M, N) bfloat16 and X (M, K) kept as MXINT8.
+
+    ``workspace``: uint8, :func:`sparq_wgrad_mx8_workspace_bytes`; needed for speed only, and only where
+    the call is captured into a graph."""
+    rc = _native.wgrad_mx8(dy, codes, scales, dw, accumulate, workspace, stream)
     if rc:
         _raise(rc)
 

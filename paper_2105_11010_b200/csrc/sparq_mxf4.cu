@@ -96,8 +96,7 @@ extern "C" int sparq_gemm_mxf4(const void *A, const uint8_t *A_scales, const voi
     if (M == 0 || N == 0) return SPARQ_OK;
     if (K == 0) return set_error(SPARQ_ERR_INVALID_ARG, "K is 0");
     if (!A || !A_scales || !B || !B_scales) return set_error(SPARQ_ERR_INVALID_ARG, "A/A_scales/B/B_scales pointer is NULL");
-    const int64_t most = INT64_C(2147483647) - 255;
-    if (M >= most || N >= most || K >= most) return set_error(SPARQ_ERR_UNSUPPORTED, "M, N and K must be below 2^31 - 256");
+    if (M >= kMxMost || N >= kMxMost || K >= kMxMost) return set_error(SPARQ_ERR_UNSUPPORTED, "M, N and K must be below 2^31 - 256");
     if (((uintptr_t)A | (uintptr_t)A_scales | (uintptr_t)B | (uintptr_t)B_scales) & 15u)
         return set_error(SPARQ_ERR_UNSUPPORTED, "codes and scales must be 16-byte aligned");
     if (((uintptr_t)e->f32_out & 3u) || ((uintptr_t)e->bf16_out & 1u) || ((uintptr_t)e->bias & 3u))

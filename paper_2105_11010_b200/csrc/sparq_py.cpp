@@ -580,11 +580,11 @@ SPARQ_PY(py_act_backward_mx8)
     });
 }
 
-// (dy, codes, scales, dw, accumulate, stream)
+// (dy, codes, scales, dw, accumulate, workspace, stream)
 SPARQ_PY(py_wgrad_mx8)
 {
     return guarded([&] {
-        Args a(args, nargs, 6);
+        Args a(args, nargs, 7);
         const Tensor &dy = a.tensor("dy"), &c = a.tensor("codes"), &s = a.tensor("scales"), &dw = a.tensor("dw");
         int dt;
         int64_t ld;
@@ -596,8 +596,11 @@ SPARQ_PY(py_wgrad_mx8)
         const uint8_t *ps = mx_scales(&s, "scales", SPARQ_MXINT8, M, K);
         float *pdw = data<float>(&dw, at::kFloat, "dw");
         const int accumulate = a.truth();
+        const Tensor *ws = a.opt("workspace");
+        uint8_t *pws = data<uint8_t>(ws, at::kByte, "workspace");
+        const size_t ws_bytes = ws ? (size_t)ws->numel() : 0;
         void *st = a.stream();
-        return call([&] { return sparq_wgrad_mx8(pdy, ld, pc, ps, M, N, K, accumulate, pdw, st); });
+        return call([&] { return sparq_wgrad_mx8(pdy, ld, pc, ps, M, N, K, accumulate, pdw, pws, ws_bytes, st); });
     });
 }
 

@@ -25,28 +25,40 @@ struct WgradForm {
     int64_t tiles;
 };
 
-// By estimates of the time in us.
+// By estimates of the time in us, fitted to launches of 64 to 100352 tokens and 64 x 256 to 2048 x 2048 outputs in every form: the choice is
+// within an eighth of the fastest.  A step of 64 tokens takes a tile 0.45 us (128 x 128, transformed on the way), 0.48 (256 x 256) and
+// 0.36 (256 x 256, expanded first).  16384 x 1024 x 1024: pairs in one part 128 us, in four 42, expanded first 89 and 40; 4096 x 128 x 1152: 128 x 128
+// 36 us, in eight parts 12.7, split in clusters of eight 11.5.
 WgradForm pick_wgrad(int64_t M, int64_t N, int64_t K, int blocks, int sms)
 {
     WgradForm best = {};
     double cost = 1e30;
     const int64_t small = (N + 127) / 128 * ((K + 127) / 128), large = (N + 255) / 256 * ((K + 255) / 256);
-    const double expand = 3.0 + (double)M * (double)K * 3.0 / 6.0e6;
+    const double expand = 1.5 + (double)M * (double)K * 3.0 / 6.0e6;
     for (int parts = 1; parts <= 128 && parts * 8 <= blocks + 7; parts += parts < 8 ? 1 : parts < 32 ? 4 : 16) {
-        const int b = (blocks + parts - 1) / parts;
-        const double join = parts > 1 ? 3.0 + (double)(parts + 1) * (double)N * (double)K * 4.0 / 5.0e6 : 0.0;
         if (parts > 1 && (double)parts * (double)N * (double)K * 4.0 > (double)kWorkspaceMaxBytes) break;
+        const int b = (blocks + parts - 1) / parts;
+        const double join = parts > 1 ? 2.5 + (double)(parts + 1) * (double)N * (double)K * 4.0 / 5.0e6 : 0.0;
         for (int split = 1; split <= 8 && split <= b; split *= 2) {
             const int64_t at_once = clusters_at_once(split, sms), rounds = (small * parts + at_once - 1) / at_once;
-            const double c = join + 0.5 + (double)rounds * (4.2 + 0.45 * ((b + split - 1) / split) + (split > 1 ? 1.5 : 0.0));
+            const double c = join + 1.0 + (double)rounds * (4.6 + 0.45 * ((b + split - 1) / split) + (split > 1 ? 1.5 : 0.0));
             if (c < cost - 0.05) { cost = c; best = {false, false, split, parts, small}; }
         }
         const int64_t rounds = (large * parts + sms / 2 - 1) / (sms / 2);
-        const double q = join + 4.5 + (double)rounds * 0.5 * b, x = join + 4.5 + expand + (double)rounds * 0.36 * b;
+        const double q = join + 7.0 + (double)rounds * 0.48 * b, x = join + 7.0 + expand + (double)rounds * 0.36 * b;
         if (q < cost - 0.05) { cost = q; best = {true, false, 1, parts, large}; }
         if (x < cost - 0.05 && (double)M * (double)mx_padded(K) * 2.0 <= (double)kWorkspaceMaxBytes) { cost = x; best = {true, true, 1, parts, large}; }
     }
     return best;
+}
+
+struct Scratch {
+    size_t x, sums;
+};
+Scratch scratch_of(const WgradForm &f, int64_t M, int64_t N, int64_t K)
+{
+    auto round = [](size_t b) { return (b + 255) / 256 * 256; };
+    return {f.expand ? round((size_t)M * (size_t)mx_padded(K) * 2) : 0, f.parts > 1 ? round((size_t)f.parts * (size_t)N * (size_t)K * sizeof(float)) : 0};
 }
 
 }  // namespace
@@ -55,15 +67,26 @@ WgradForm pick_wgrad(int64_t M, int64_t N, int64_t K, int blocks, int sms)
 
 using namespace sparq;
 
+extern "C" int64_t sparq_wgrad_mx8_workspace_bytes(int64_t M, int64_t N, int64_t K)
+{
+    if (M < 0 || N < 0 || K < 0) return set_error(SPARQ_ERR_INVALID_ARG, "negative dimension");
+    if (M >= kMxMost || N >= kMxMost || K >= kMxMost) return set_error(SPARQ_ERR_UNSUPPORTED, "M, N and K must be below 2^31 - 256");
+    if (M == 0 || N == 0 || K == 0) return 0;
+    int sms = 0;
+    const int rc = device_info(&sms);
+    if (rc != SPARQ_OK) return rc;
+    const Scratch need = scratch_of(pick_wgrad(M, N, K, (int)((M + kWgTokens - 1) / kWgTokens), sms), M, N, K);
+    return (int64_t)(need.x + need.sums);
+}
+
 extern "C" int sparq_wgrad_mx8(const void *dy, int64_t lddy, const int8_t *codes, const uint8_t *scales,
-                               int64_t M, int64_t N, int64_t K, int accumulate, float *dw, void *stream)
+                               int64_t M, int64_t N, int64_t K, int accumulate, float *dw, void *workspace, size_t workspace_bytes, void *stream)
 {
     if (M < 0 || N < 0 || K < 0) return set_error(SPARQ_ERR_INVALID_ARG, "negative dimension");
     if (N == 0 || K == 0) return SPARQ_OK;
     if (!dw) return set_error(SPARQ_ERR_INVALID_ARG, "dw is NULL");
     if ((uintptr_t)dw & 3u) return set_error(SPARQ_ERR_UNSUPPORTED, "dw must be 4-byte aligned");
-    const int64_t most = INT64_C(2147483647) - 255;
-    if (M >= most || N >= most || K >= most) return set_error(SPARQ_ERR_UNSUPPORTED, "M, N and K must be below 2^31 - 256");
+    if (M >= kMxMost || N >= kMxMost || K >= kMxMost) return set_error(SPARQ_ERR_UNSUPPORTED, "M, N and K must be below 2^31 - 256");
     cudaStream_t st = (cudaStream_t)stream;
     if (M == 0) {           // a sum over no tokens
         if (accumulate) return SPARQ_OK;
@@ -94,14 +117,19 @@ extern "C" int sparq_wgrad_mx8(const void *dy, int64_t lddy, const int8_t *codes
     if ((rc = encode_matrix(&map_codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, pitch, M, pitch, kWgBN, kWgTokens, CU_TENSOR_MAP_SWIZZLE_128B)) != SPARQ_OK) return rc;
     if ((rc = encode_matrix(&map_scales, CU_TENSOR_MAP_DATA_TYPE_UINT8, scales, spitch, M, spitch, 16, kWgTokens, CU_TENSOR_MAP_SWIZZLE_NONE)) != SPARQ_OK) return rc;
     const WgradForm form = pick_wgrad(M, N, K, g.blocks, sms);
+    const Scratch need = scratch_of(form, M, N, K);
+    if (workspace && ((uintptr_t)workspace & 255u)) return set_error(SPARQ_ERR_UNSUPPORTED, "workspace must be 256-byte aligned");
+    if (workspace && workspace_bytes < need.x + need.sums)
+        return set_error(SPARQ_ERR_INVALID_ARG, "workspace of %zu bytes, %zu are needed", workspace_bytes, need.x + need.sums);
     g.parts = form.parts;
     g.split = form.split;
     if (form.tiles * form.parts * form.split > INT64_C(1) << 30) return set_error(SPARQ_ERR_UNSUPPORTED, "more than 2^30 tiles");
-    // Scratch memory for X in bf16 and for the parts' sums.  Without it (a stream that is being captured) X is expanded stage by stage and
-    // the parts add to dw one launch after the other: the same sums in the same order.
+    // Memory for X in bf16 and for the parts' sums: the caller's, else scratch.  Without any (a stream that is being captured) X is expanded
+    // stage by stage and the parts add to dw one launch after the other: the same sums in the same order.
     CUtensorMap map_x;
-    void *x = form.expand ? workspace_alloc((size_t)M * (size_t)pitch * 2, st) : nullptr;
-    float *sums = form.parts > 1 ? (float *)workspace_alloc((size_t)form.parts * (size_t)N * (size_t)K * sizeof(float), st) : nullptr;
+    void *const own = !workspace && need.x ? workspace_alloc(need.x, st) : nullptr, *const own_sums = !workspace && need.sums ? workspace_alloc(need.sums, st) : nullptr;
+    void *const x = workspace && need.x ? workspace : own;
+    float *const sums = (float *)(workspace && need.sums ? (uint8_t *)workspace + need.x : own_sums);
     rc = SPARQ_OK;
     if (x) {
         rc = sparq_dequantize_mx(codes, scales, M, K, SPARQ_MXINT8, nullptr, x, SPARQ_DTYPE_BF16, pitch, stream);
@@ -137,7 +165,7 @@ extern "C" int sparq_wgrad_mx8(const void *dy, int64_t lddy, const int8_t *codes
                                                 g.parts, (int)(accumulate != 0), dw);
         if (e != cudaSuccess) rc = cuda_error(e, "wgrad_add_parts_kernel launch");
     }
-    workspace_free(sums, st);
-    workspace_free(x, st);
+    workspace_free(own_sums, st);
+    workspace_free(own, st);
     return rc;
 }

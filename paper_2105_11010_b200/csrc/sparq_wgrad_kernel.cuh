@@ -636,12 +636,12 @@ sparq_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_cons
     tc_fence_after();
     c.tmem = tmem_base_slot;
     dep_wait();
-    // Registers: 384 threads were launched with 168 each; of the same 64512, the workers take 216 and the first four warps 72.
+    // Registers: 384 threads were launched with 168 each; of the same 64512, the workers take 224 and the first four warps 56.
     if (warp >= kWgFirstWorker) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         c.work(p);
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         switch (warp) {
         case 0: c.template produce<true>(map_dy, map_dy, p); break;
         case 1: c.issue(p); break;

@@ -114,7 +114,7 @@ def test_wgrad():
     L = sparq.load_library()
 
     def call(dy=P, ld=64, codes=P, scales=P, M=4, N=64, K=64, acc=0, dw=P):
-        return L.sparq_wgrad_mx8(dy, ld, codes, scales, M, N, K, acc, dw, None)
+        return L.sparq_wgrad_mx8(dy, ld, codes, scales, M, N, K, acc, dw, None, 0, None)
     refused(-1, "negative", call(K=-1))
     refused(-1, "dw", call(dw=None))
     refused(-2, "aligned", call(dw=P + 2))
@@ -126,6 +126,9 @@ def test_wgrad():
     refused(-2, "multiple of 8", call(ld=68))
     refused(-2, "multiple of 8", call(dy=P + 8))
     refused(-2, "aligned", call(codes=P + 4))
+    refused(-1, "negative", L.sparq_wgrad_mx8_workspace_bytes(4, -1, 4))
+    refused(-2, "2^31", L.sparq_wgrad_mx8_workspace_bytes(4, 1 << 31, 4))
+    assert L.sparq_wgrad_mx8_workspace_bytes(0, 4, 4) == 0
     assert call(N=0, dw=None) == 0 and call(K=0, dw=None) == 0 and call(M=0, acc=1, dy=None) == 0
 
 
