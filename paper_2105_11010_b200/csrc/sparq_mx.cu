@@ -48,7 +48,7 @@ quantize_mx_kernel(const void *x, int64_t rows, int64_t cols, int64_t ldx, uint3
 {
     constexpr int kWidth = BF16 ? 2 : 4;
     const int64_t stride = (int64_t)gridDim.x * kRunThreads, first = (int64_t)blockIdx.x * kRunThreads + threadIdx.x;
-    const int64_t pitch = mx_code_pitch(FORMAT, cols), words = mx_scale_cols(FORMAT, cols) / 4;
+    const int64_t pitch = mx_code_pitch(FORMAT, cols), spitch = mx_scale_cols(FORMAT, cols);
     const uint32_t coded = (uint32_t)(mx_padded(cols) / 16);
     const Span span = span_of<BF16>(x, rows, cols, ldx);
     RunWalk at(first, stride, per_row);
@@ -60,9 +60,9 @@ quantize_mx_kernel(const void *x, int64_t rows, int64_t cols, int64_t ldx, uint3
         enc = __fdiv_rn(2688.0f, m);
         enc_scale = __fdiv_rn(448.0f, m);
     }
-    // `runs` is a multiple of 32: a warp's lanes leave the loop together
-    for (int64_t i = first; i < runs; i += stride, at.next()) {
-        const int64_t left = at.row < rows ? cols - (int64_t)at.run * 16 : 0;
+    // a warp's lanes leave the loop together; those past the last run have nothing to read or write
+    for (int64_t i = first; i < ((runs + 31) & ~INT64_C(31)); i += stride, at.next()) {
+        const int64_t left = i < runs && at.row < rows ? cols - (int64_t)at.run * 16 : 0;
         uint32_t v[kRunWords<BF16>];
         load_words<BF16, ALIGN>(v, reinterpret_cast<const uint8_t *>(x) + (left > 0 ? (at.row * ldx + at.run * 16) * kWidth : 0), left, span);
         uint32_t mb = run_max_bits<BF16>(v);
@@ -80,7 +80,7 @@ quantize_mx_kernel(const void *x, int64_t rows, int64_t cols, int64_t ldx, uint3
             if (FORMAT == SPARQ_MXFP4) mul = inv_pow2_of_code(code);
         }
         const bool none = mb >= kInfBits || mul == 0.0f;      // a scale that is zero or NaN: codes of zero
-        const bool live = at.row < rows && at.run < coded;
+        const bool live = i < runs && at.row < rows && at.run < coded;
         if (live) {
             uint8_t *dst = codes + at.row * pitch;
             if (FORMAT == SPARQ_MXINT8) {
@@ -93,11 +93,15 @@ quantize_mx_kernel(const void *x, int64_t rows, int64_t cols, int64_t ldx, uint3
                 reinterpret_cast<uint2 *>(dst)[at.run] = none ? make_uint2(0u, 0u) : make_uint2(lo, hi);
             }
         }
-        // four scales at a time, the padding's too: zero, which is a number in either format
-        constexpr int kLanes = FORMAT == SPARQ_NVFP4 ? 4 : 8;
-        const uint32_t word = gather_word<kLanes>(live ? code : 0u);
-        if ((threadIdx.x & (kLanes - 1)) == 0)
-            *reinterpret_cast<uint32_t *>(scales + mx_scale_word<FORMAT != SPARQ_MXINT8>(at.row, at.run / kLanes, words)) = word;
+        if (FORMAT == SPARQ_MXINT8) {
+            if (i < runs) put_int8_scale(scales, at.row, at.run, per_row, spitch, code);
+        } else {
+            // four scales at a time, the padding's too: zero, which is a number in either format.  (Whole words: runs are a multiple of 32.)
+            constexpr int kLanes = FORMAT == SPARQ_NVFP4 ? 4 : 8;
+            const uint32_t word = gather_word<kLanes>(live ? code : 0u);
+            if ((threadIdx.x & (kLanes - 1)) == 0)
+                *reinterpret_cast<uint32_t *>(scales + mx_scale_at<true>(at.row, at.run / kLanes * 4, spitch)) = word;
+        }
     }
 }
 
@@ -108,7 +112,7 @@ dequantize_mx_kernel(const uint8_t *codes, const uint8_t *scales, int64_t rows, 
 {
     constexpr int kWidth = BF16 ? 2 : 4;
     const int64_t stride = (int64_t)gridDim.x * kRunThreads, first = (int64_t)blockIdx.x * kRunThreads + threadIdx.x;
-    const int64_t pitch = mx_code_pitch(FORMAT, cols), words = mx_scale_cols(FORMAT, cols) / 4, runs = rows * per_row;
+    const int64_t pitch = mx_code_pitch(FORMAT, cols), spitch = mx_scale_cols(FORMAT, cols), runs = rows * per_row;
     RunWalk at(first, stride, per_row);
     dep_wait();
     dep_launch();
@@ -120,7 +124,7 @@ dequantize_mx_kernel(const uint8_t *codes, const uint8_t *scales, int64_t rows, 
         int64_t left = 0;
         if (i < runs) {
             const uint32_t c = FORMAT == SPARQ_NVFP4 ? at.run : at.run >> 1;
-            const uint32_t code = scales[mx_scale_word<FORMAT != SPARQ_MXINT8>(at.row, c >> 2, words) + (c & 3)];
+            const uint32_t code = scales[mx_scale_at<FORMAT != SPARQ_MXINT8>(at.row, c, spitch)];
             const uint8_t *src = codes + at.row * pitch;
             left = cols - (int64_t)at.run * 16;
             if (FORMAT == SPARQ_MXINT8) {
@@ -189,7 +193,7 @@ extern "C" int sparq_quantize_mx(const void *x, int dtype, int64_t rows, int64_t
     if (rc == SPARQ_OK) rc = check_tensor(dtype, rows, cols, ldx, x, codes, scales, "x");
     if (rc != SPARQ_OK || rows == 0 || cols == 0) return rc;
     const bool bf16 = dtype == SPARQ_DTYPE_BF16;
-    const uint32_t per_row = (uint32_t)(mx_scale_cols(format, cols) * (mx_block(format) / 16));
+    const uint32_t per_row = (uint32_t)mx_runs(format, cols);
     const int64_t runs = mx_scale_rows(format, rows) * per_row;
     int blocks = 0;
     if ((rc = run_grid(runs, &blocks)) != SPARQ_OK) return rc;

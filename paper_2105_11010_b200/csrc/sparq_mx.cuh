@@ -28,12 +28,17 @@ SPARQ_HD int64_t mx_scale_cols(int format, int64_t cols)
 }
 SPARQ_HD int64_t mx_scale_rows(int format, int64_t rows) { return format == SPARQ_MXINT8 ? rows : round_up64(rows, 128); }
 
-// Word w (scales 4w .. 4w + 3) of row r.
+// Scale c of row r; `pitch` = mx_scale_cols.
 template <bool TILED>
-__host__ __device__ __forceinline__ int64_t mx_scale_word(int64_t row, int64_t w, int64_t words)
+__host__ __device__ __forceinline__ int64_t mx_scale_at(int64_t row, int64_t c, int64_t pitch)
 {
-    if (!TILED) return (row * words + w) * 4;
-    return ((row >> 7) * words + w) * 512 + (row & 31) * 16 + ((row >> 5) & 3) * 4;
+    if (!TILED) return row * pitch + c;
+    return ((row >> 7) * (pitch >> 2) + (c >> 2)) * 512 + (row & 31) * 16 + ((row >> 5) & 3) * 4 + (c & 3);
+}
+// Runs of 16 elements that a row's walk takes: its coded ones, and those of a tile's padding.
+SPARQ_HD int64_t mx_runs(int format, int64_t cols)
+{
+    return format == SPARQ_MXINT8 ? mx_padded(cols) / 16 : mx_scale_cols(format, cols) * (mx_block(format) / 16);
 }
 
 // Checks shared by the entry points (sparq_mx.cu).
@@ -329,6 +334,15 @@ __device__ __forceinline__ void floats_of_int8(float (&f)[16], uint4 codes, uint
 #pragma unroll
         for (int i = 0; i < 4; ++i) f[4 * j + i] = __fmul_rn(__fadd_rn(__uint_as_float(prmt(u, 0x4B000000u, 0x7540u + i)), -8388736.0f), s);
     }
+}
+
+// MXINT8 scales of a warp's runs, each block's in two neighbouring lanes; the last run of a row clears the padding behind it.
+__device__ __forceinline__ void put_int8_scale(uint8_t *scales, uint32_t row, uint32_t run, uint32_t per_row, int64_t pitch, uint32_t code)
+{
+    uint8_t *at = scales + (int64_t)row * pitch;
+    if ((run & 1u) == 0) at[run >> 1] = (uint8_t)code;
+    if (run == per_row - 1)
+        for (int64_t c = per_row >> 1; c < pitch; ++c) at[c] = 0;
 }
 
 // A warp's four (eight) neighbouring lanes hold a scale each (each twice): the word of the four, valid in the

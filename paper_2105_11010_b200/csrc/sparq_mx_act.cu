@@ -59,21 +59,19 @@ __device__ __forceinline__ void act_both(float x, float &y, float &d)
 
 // Codes and scale of a run, its block's other half in the neighbouring lane.
 template <bool BF16>
-__device__ __forceinline__ void keep_run(const uint32_t (&v)[kRunWords<BF16>], const float (&x)[16], bool coded, uint32_t row, uint32_t run, int64_t pitch,
-                                         int64_t words, int8_t *codes, uint8_t *scales)
+__device__ __forceinline__ void keep_run(const uint32_t (&v)[kRunWords<BF16>], const float (&x)[16], bool live, const RunWalk &at, int64_t pitch,
+                                         int64_t spitch, int8_t *codes, uint8_t *scales)
 {
     uint32_t mb = run_max_bits<BF16>(v);
     mb = max(mb, __shfl_xor_sync(0xFFFFFFFFu, mb, 1));
+    if (!live) return;
     const uint32_t code = e8m0_code(mb, 0u);
-    if (coded) {
-        float f[16];
+    float f[16];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) f[j] = x[j];
-        const uint4 w = int8_codes(f, code, mb);
-        reinterpret_cast<uint4 *>(codes + row * pitch)[run] = mb >= kInfBits ? make_uint4(0u, 0u, 0u, 0u) : w;
-    }
-    const uint32_t word = gather_word<8>(coded ? code : 0u);
-    if ((threadIdx.x & 7) == 0) *reinterpret_cast<uint32_t *>(scales + mx_scale_word<false>(row, run >> 3, words)) = word;
+    for (int j = 0; j < 16; ++j) f[j] = x[j];
+    const uint4 w = int8_codes(f, code, mb);
+    reinterpret_cast<uint4 *>(codes + at.row * pitch)[at.run] = mb >= kInfBits ? make_uint4(0u, 0u, 0u, 0u) : w;
+    put_int8_scale(scales, at.row, at.run, at.per_row, spitch, code);
 }
 
 struct ActForward {
@@ -91,24 +89,24 @@ act_forward_mx8_kernel(const ActForward g)
 {
     constexpr int kWidth = BF16 ? 2 : 4;
     const int64_t stride = (int64_t)gridDim.x * kRunThreads, first = (int64_t)blockIdx.x * kRunThreads + threadIdx.x;
-    const int64_t pitch = mx_padded(g.cols), words = mx_scale_cols(SPARQ_MXINT8, g.cols) / 4, runs = g.rows * g.per_row;
+    const int64_t pitch = mx_padded(g.cols), spitch = mx_scale_cols(SPARQ_MXINT8, g.cols), runs = g.rows * g.per_row;
     RunWalk at(first, stride, g.per_row);
     dep_wait();
     dep_launch();
     const Span sx = span_of<BF16>(g.x, g.rows, g.cols, g.ldx), su = span_of<BF16>(g.up, g.rows, g.cols, g.ldx);
-    // per_row is a multiple of 32: a warp's lanes share a row and leave the loop together
-    for (int64_t i = first; i < runs; i += stride, at.next()) {
-        const int64_t left = g.cols - (int64_t)at.run * 16, off = left > 0 ? (at.row * g.ldx + at.run * 16) * kWidth : 0;
-        const bool coded = (int64_t)at.run * 16 < pitch;
+    // a warp's lanes leave the loop together; those past the last run have nothing to read or write
+    for (int64_t i = first; i < ((runs + 31) & ~INT64_C(31)); i += stride, at.next()) {
+        const bool live = i < runs;
+        const int64_t left = live ? g.cols - (int64_t)at.run * 16 : 0, off = left > 0 ? (at.row * g.ldx + at.run * 16) * kWidth : 0;
         uint32_t vx[kRunWords<BF16>], vu[kRunWords<BF16>];
         load_words<BF16, ALIGN>(vx, reinterpret_cast<const uint8_t *>(g.x) + off, left, sx);
         if (GATED) load_words<BF16, ALIGN>(vu, reinterpret_cast<const uint8_t *>(g.up) + off, left, su);
         float f[16], u[16];
         floats_of_words<BF16>(f, vx);
-        keep_run<BF16>(vx, f, coded, at.row, at.run, pitch, words, g.codes, g.scales);
+        keep_run<BF16>(vx, f, live, at, pitch, spitch, g.codes, g.scales);
         if (GATED) {
             floats_of_words<BF16>(u, vu);
-            keep_run<BF16>(vu, u, coded, at.row, at.run, pitch, words, g.up_codes, g.up_scales);
+            keep_run<BF16>(vu, u, live, at, pitch, spitch, g.up_codes, g.up_scales);
         }
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
@@ -134,7 +132,7 @@ act_backward_mx8_kernel(const ActBackward g)
 {
     constexpr int kWidth = BF16 ? 2 : 4;
     const int64_t stride = (int64_t)gridDim.x * kRunThreads, first = (int64_t)blockIdx.x * kRunThreads + threadIdx.x;
-    const int64_t pitch = mx_padded(g.cols), words = mx_scale_cols(SPARQ_MXINT8, g.cols) / 4, runs = g.rows * g.per_row;
+    const int64_t pitch = mx_padded(g.cols), spitch = mx_scale_cols(SPARQ_MXINT8, g.cols), runs = g.rows * g.per_row;
     RunWalk at(first, stride, g.per_row);
     dep_wait();
     dep_launch();
@@ -145,7 +143,7 @@ act_backward_mx8_kernel(const ActBackward g)
         int64_t left = 0;
         if (i < runs) {
             left = g.cols - (int64_t)at.run * 16;
-            const int64_t sc = mx_scale_word<false>(at.row, at.run >> 3, words) + ((at.run >> 1) & 3);
+            const int64_t sc = mx_scale_at<false>(at.row, at.run >> 1, spitch);
             uint32_t v[kRunWords<BF16>];
             float x[16];
             load_words<BF16, ALIGN>(v, reinterpret_cast<const uint8_t *>(g.dy) + (at.row * g.lddy + at.run * 16) * kWidth, left, sdy);
@@ -224,7 +222,7 @@ extern "C" int sparq_act_forward_mx8(const void *x, const void *up, int dtype, i
     const bool bf16 = dtype == SPARQ_DTYPE_BF16;
     const int width = bf16 ? 2 : 4;
     const int align = min_align(min_align(run_align(x, ldx, width), run_align(y, ldy, width)), up ? run_align(up, ldx, width) : 32);
-    const ActForward g = {x, up, rows, cols, ldx, ldy, (uint32_t)(2 * mx_scale_cols(SPARQ_MXINT8, cols)), y, codes, up_codes, scales, up_scales};
+    const ActForward g = {x, up, rows, cols, ldx, ldy, (uint32_t)mx_runs(SPARQ_MXINT8, cols), y, codes, up_codes, scales, up_scales};
     int blocks = 0;
     if ((rc = run_grid(rows * g.per_row, &blocks)) != SPARQ_OK) return rc;
     const auto kernel = SPARQ_ACT_PICK(act_forward_mx8_kernel, bf16, align, act, up != nullptr);

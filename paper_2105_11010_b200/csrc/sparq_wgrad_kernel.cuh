@@ -97,6 +97,61 @@ __device__ __forceinline__ void transform_stage(uint32_t at, const TeamPlace &p)
 // the other half of the accumulators.
 constexpr int kWgChunkSteps = 8;                 // 512 tokens
 
+// C columns of a row (sum[at(j)] is column j) to `out`, the first `cols` of them, added to what is there or not.  Whole vectors
+// where they can be: 32 bytes, or behind the row's first 16-byte boundary 16 (rows of a length that is no multiple of four, element by
+// element: 316 x 2496 x 3779 67 us).
+template <int C, class At>
+__device__ __forceinline__ void wgrad_put_row(float *out, const float (&sum)[C], int64_t cols, int accumulate, At at)
+{
+    if (cols >= C && (reinterpret_cast<uintptr_t>(out) & 31u) == 0) {
+#pragma unroll
+        for (int j = 0; j < C; j += 8) {
+            uint32_t v[8];
+            if (accumulate) {
+                ld_v8(v, out + j);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = __float_as_uint(__fadd_rn(__uint_as_float(v[i]), sum[at(j + i)]));
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = __float_as_uint(sum[at(j + i)]);
+            }
+            st_v8(out + j, v);
+        }
+        return;
+    }
+    auto one = [&](int64_t j, float v) { out[j] = accumulate ? __fadd_rn(out[j], v) : v; };
+    // columns head .. head + 3, + 4 .. + 7 and so on are vectors; head differs from lane to lane
+    const int head = (int)((0u - ((uint32_t)reinterpret_cast<uintptr_t>(out) >> 2)) & 3u);
+#pragma unroll
+    for (int j = 0; j < 3; ++j)
+        if (j < head && j < cols) one(j, sum[at(j)]);
+#pragma unroll
+    for (int j = 0; j < C; j += 4) {
+        float t[6], v[4];
+#pragma unroll
+        for (int i = 0; i < 6; ++i) {
+            const float a = j + i < C ? sum[at((j + i) % C)] : 0.0f, b = j + i + 1 < C ? sum[at((j + i + 1) % C)] : 0.0f;
+            t[i] = head & 1 ? b : a;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = head & 2 ? t[i + 2] : t[i];
+        const int64_t first = j + head;
+        if (j + 4 <= C - 4 + (head == 0 ? 4 : 0) && first + 4 <= cols) {
+            float4 *to = reinterpret_cast<float4 *>(out + first);
+            float4 w = make_float4(v[0], v[1], v[2], v[3]);
+            if (accumulate) {
+                const float4 o = *to;
+                w = make_float4(__fadd_rn(o.x, w.x), __fadd_rn(o.y, w.y), __fadd_rn(o.z, w.z), __fadd_rn(o.w, w.w));
+            }
+            *to = w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (first + i < cols && first + i < C) one(first + i, v[i]);
+        }
+    }
+}
+
 // ---- few output tiles, or little work ------------------------------------------------------------------
 // Tiles of 128 x 128, a cluster of `split` CTAs on each that take equal runs of tokens: their partial sums go to the CTA that
 // owns a group of four columns through distributed shared memory (the operand ring's, once every CTA of the cluster is
@@ -248,21 +303,21 @@ struct WgradSmall : MxCta {
             for (int j = 0; j < 4; ++j)
                 if (col + j < cols) out[j] = g.accumulate ? out[j] + a[j] : a[j];
         };
+        if (split == 1) {
+            if (n < g.N && half * kWgOwn < cols)
+                wgrad_put_row(dw + n * g.K + k0 + half * kWgOwn, sum, cols - half * kWgOwn, g.accumulate, [](int j) { return wgrad_column(j); });
+            return;
+        }
 #pragma unroll
         for (int q = 0; q < kWgOwn / 4; ++q) {
             const int grp = half * (kWgOwn / 4) + q;
             if (grp >= groups) continue;
             const float a[4] = {sum[4 * q], sum[4 * q + wgrad_column(1)], sum[4 * q + wgrad_column(2)], sum[4 * q + 3]};
-            if (split == 1) {
-                put(grp * 4, a);
-            } else {
-                const int owner = grp / own, local = grp - owner * own;
-                const uint32_t dst = smem + (uint32_t)(((rank * own + local) * 128 + quarter * 32 + lane) * 16);
-                store_remote16(map_to_rank(dst, owner), map_to_rank(recv_bar(), owner), __float_as_uint(a[0]), __float_as_uint(a[1]),
-                               __float_as_uint(a[2]), __float_as_uint(a[3]));
-            }
+            const int owner = grp / own, local = grp - owner * own;
+            const uint32_t dst = smem + (uint32_t)(((rank * own + local) * 128 + quarter * 32 + lane) * 16);
+            store_remote16(map_to_rank(dst, owner), map_to_rank(recv_bar(), owner), __float_as_uint(a[0]), __float_as_uint(a[1]),
+                           __float_as_uint(a[2]), __float_as_uint(a[3]));
         }
-        if (split == 1) return;
         mbar_wait(recv_bar(), 0, abort_flag, g.status, g.wait_limit, true);
         for (int local = half; local < own_valid; local += 2) {
             float a[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -523,28 +578,7 @@ struct WgradPair : MxCta {
 
     __device__ void write(const WgradArgs &g, float *dw, int64_t n, int64_t k, const float (&sum)[kWgPairOwn]) const
     {
-        if (n >= g.N) return;
-        float *out = dw + n * g.K + k;
-        auto at = [](int j) { return X16 ? j : wgrad_column(j); };       // of column j in the accumulator
-        if (k + kWgPairOwn <= g.K && (reinterpret_cast<uintptr_t>(out) & 31u) == 0) {
-#pragma unroll
-            for (int j = 0; j < kWgPairOwn; j += 8) {
-                uint32_t v[8];
-                if (g.accumulate) {
-                    ld_v8(v, out + j);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] = __float_as_uint(__fadd_rn(__uint_as_float(v[i]), sum[at(j + i)]));
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] = __float_as_uint(sum[at(j + i)]);
-                }
-                st_v8(out + j, v);
-            }
-            return;
-        }
-#pragma unroll
-        for (int j = 0; j < kWgPairOwn; ++j)
-            if (k + j < g.K) out[j] = g.accumulate ? __fadd_rn(out[j], sum[at(j)]) : sum[at(j)];
+        if (n < g.N && k < g.K) wgrad_put_row(dw + n * g.K + k, sum, g.K - k, g.accumulate, [](int j) { return X16 ? j : wgrad_column(j); });
     }
 
     __device__ void work(const WgradPairArgs &p) const
