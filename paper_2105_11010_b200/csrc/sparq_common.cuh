@@ -31,6 +31,9 @@ int validate_params(const sparq_params *p, XformArgs *x);
 // SPARQ_OK for SPARQ_DTYPE_F32 and SPARQ_DTYPE_BF16 (sparq_frontend.cu).
 int check_dtype(int dtype);
 
+// SMs of the current device, which must be an sm_100 (sparq_gemm.cu).
+int device_info(int *sms);
+
 // Device status word shared by all kernels of this library on the current device.
 // Bit 0: a bounded wait expired.  Allocated on first use, freed by sparq_shutdown().
 int get_status_word(unsigned int **dptr);

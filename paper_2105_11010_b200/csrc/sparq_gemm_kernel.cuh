@@ -59,9 +59,8 @@ constexpr int kSmemBudget = 200 * 1024;  // for the stage ring
 // kernel argument, so that a diagnostic launch can make a wait run out in microseconds.
 constexpr long long kWaitLimitCycles = 2000000000LL;
 
-// Host side, shared by the contractions (sparq_gemm.cu): the SMs of the current device, which must be an sm_100, and a
-// tensor map (encoded once per set of arguments) of a matrix that is read in boxes.
-int device_info(int *sms);
+// Host side, shared by the contractions (sparq_gemm.cu): a tensor map (encoded once per set of arguments) of a matrix that is
+// read in boxes, and of a 4-bit operand's scales.
 int encode_matrix(CUtensorMap *map, CUtensorMapDataType type, const void *ptr, int64_t inner, int64_t rows, int64_t pitch, int box_inner,
                   int box_rows, CUtensorMapSwizzle swizzle);
 int encode_scale_tiles(CUtensorMap *map, const void *ptr, int64_t tiles, int64_t blocks, int box_tiles, int box_blocks);

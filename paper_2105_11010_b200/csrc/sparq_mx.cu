@@ -30,10 +30,9 @@ int check_mx_extent(int64_t rows, int64_t cols, int64_t ld)
 
 int run_grid(int64_t runs, int *blocks)
 {
-    int dev = 0, sms = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-    if (e != cudaSuccess) return cuda_error(e, "device query");
+    int sms = 0;
+    const int rc = device_info(&sms);
+    if (rc != SPARQ_OK) return rc;
     const int64_t want = (runs + kRunThreads - 1) / kRunThreads, cap = (int64_t)sms * 32;
     *blocks = (int)(want < cap ? want : cap);
     return SPARQ_OK;
