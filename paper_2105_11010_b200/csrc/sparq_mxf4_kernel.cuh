@@ -108,26 +108,23 @@ struct Mxf4Pair : MxCta {
                 for (int kb = 0; kb < g.k_blocks; ++kb) {
                     mbar_wait(full_bar(s), ph, abort_flag, g.status, g.wait_limit);
                     tc_fence_after();
-                    if (elected) {
-                        const uint32_t at = smem + (uint32_t)(s * kRoom), sf = at + kScalesAt, ta = tmem + kPairScales, tb = ta + 4 * T;
-                        const uint64_t adesc = make_smem_desc<kMxBK>(at), bdesc = make_smem_desc<kMxBK>(at + kHalf);
-                        const int mmas = g.k_mmas - kb * kMxSteps;
+                    const uint32_t at = smem + (uint32_t)(s * kRoom), sf = at + kScalesAt, ta = tmem + kPairScales, tb = ta + 4 * T;
+                    const uint64_t adesc = make_smem_desc<kMxBK>(at), bdesc = make_smem_desc<kMxBK>(at + kHalf);
+                    const int mmas = g.k_mmas - kb * kMxSteps;
 #pragma unroll
-                        for (int k = 0; k < kMxSteps; ++k) {
-                            if (k >= mmas) continue;
-                            const int q = NV ? k : k >> 1;
-                            if (NV || (k & 1) == 0) {
-                                tc_copy_scales_pair(ta + 4 * q, scale_desc(sf + q * kScaleTile));
-                                tc_copy_scales_pair(tb + 8 * q, scale_desc(sf + (T + q) * kScaleTile));
-                                tc_copy_scales_pair(tb + 8 * q + 4, scale_desc(sf + (2 * T + q) * kScaleTile));
-                            }
-                            tc_mma_f4_pair<NV>(d, adesc + (uint64_t)(k * 2), bdesc + (uint64_t)(k * 2), make_idesc_f4(kPairTile, 256, NV, NV ? 0u : (k & 1) * 2u),
-                                               ta + 4 * q, tb + 8 * q, (kb > 0 || k > 0) ? 1u : 0u);
+                    for (int k = 0; k < kMxSteps; ++k) {
+                        if (k >= mmas) continue;
+                        const int q = NV ? k : k >> 1;
+                        if (NV || (k & 1) == 0) {
+                            tc_copy_scales_pair(ta + 4 * q, scale_desc(sf + q * kScaleTile), elected);
+                            tc_copy_scales_pair(tb + 8 * q, scale_desc(sf + (T + q) * kScaleTile), elected);
+                            tc_copy_scales_pair(tb + 8 * q + 4, scale_desc(sf + (2 * T + q) * kScaleTile), elected);
                         }
-                        tc_commit_pair(empty_bar(s));
-                        if (kb == g.k_blocks - 1) tc_commit_pair(acc_bar(i & 1));
+                        tc_mma_f4_pair<NV>(d, adesc + (uint64_t)(k * 2), bdesc + (uint64_t)(k * 2), make_idesc_f4(kPairTile, 256, NV, NV ? 0u : (k & 1) * 2u),
+                                           ta + 4 * q, tb + 8 * q, (kb > 0 || k > 0) ? 1u : 0u, elected);
                     }
-                    __syncwarp();
+                    tc_commit_pair(empty_bar(s), elected);
+                    if (kb == g.k_blocks - 1) tc_commit_pair(acc_bar(i & 1), elected);
                     if (++s == kStages) { s = 0; ph ^= 1u; }
                 }
             }

@@ -215,28 +215,24 @@ struct Mxf4Small : MxCta {
         for (int it = 0; it < steps; ++it) {
             mbar_wait(full_bar(s), ph, abort_flag, g.status, g.wait_limit);
             tc_fence_after();
-            if (elected) {
-                const uint32_t at = smem + (uint32_t)(s * kStage), sf = at + kScalesAt;
-                const int mmas = g.k_mmas - (kb_first + it) * kMxSteps;
-                const uint64_t rdesc = make_smem_desc<kMxBK>(at), cdesc = make_smem_desc<kMxBK>(at + kRows);
+            const uint32_t at = smem + (uint32_t)(s * kStage), sf = at + kScalesAt;
+            const int mmas = g.k_mmas - (kb_first + it) * kMxSteps;
+            const uint64_t rdesc = make_smem_desc<kMxBK>(at), cdesc = make_smem_desc<kMxBK>(at + kRows);
 #pragma unroll
-                for (int k = 0; k < kMxSteps; ++k) {
-                    if (k >= mmas) continue;
-                    const int t = NV ? k : k >> 1;
-                    if (NV || (k & 1) == 0) {
-                        tc_copy_scales(tmem + kColsR + 4 * t, scale_desc(sf + t * kScaleTile));
-                        tc_copy_scales(tmem + kColsC + 4 * t, scale_desc(sf + (T + t) * kScaleTile));
-                    }
-                    tc_mma_f4<NV>(tmem, rdesc + (uint64_t)(k * 2), cdesc + (uint64_t)(k * 2), make_idesc_f4(BN, 128, NV, NV ? 0u : (k & 1) * 2u),
-                                  tmem + kColsR + 4 * t, tmem + kColsC + 4 * t, (it > 0 || k > 0) ? 1u : 0u);
+            for (int k = 0; k < kMxSteps; ++k) {
+                if (k >= mmas) continue;
+                const int t = NV ? k : k >> 1;
+                if (NV || (k & 1) == 0) {
+                    tc_copy_scales(tmem + kColsR + 4 * t, scale_desc(sf + t * kScaleTile), elected);
+                    tc_copy_scales(tmem + kColsC + 4 * t, scale_desc(sf + (T + t) * kScaleTile), elected);
                 }
-                tc_commit(empty_bar(s));
+                tc_mma_f4<NV>(tmem, rdesc + (uint64_t)(k * 2), cdesc + (uint64_t)(k * 2), make_idesc_f4(BN, 128, NV, NV ? 0u : (k & 1) * 2u),
+                              tmem + kColsR + 4 * t, tmem + kColsC + 4 * t, (it > 0 || k > 0) ? 1u : 0u, elected);
             }
-            __syncwarp();
+            tc_commit_if(empty_bar(s), elected);
             if (++s == S) { s = 0; ph ^= 1u; }
         }
-        if (elected) tc_commit(acc_bar());
-        __syncwarp();
+        tc_commit_if(acc_bar(), elected);
         mbar_wait(acc_bar(), 0, abort_flag, g.status, g.wait_limit, true);
         __syncwarp();
     }

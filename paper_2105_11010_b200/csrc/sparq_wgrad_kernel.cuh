@@ -61,7 +61,7 @@ __host__ __device__ constexpr int wgrad_column(int j) { return (j & ~3) | ((j & 
 // columns).  A thread takes 16 codes of every sixteenth token.  Eight neighbouring lanes take half a row each of tokens t and t ^ 5, whose
 // swizzles differ in bits 0 and 2: loads and stores of 16 bytes then meet all banks.  All loads go out before the first store.
 struct TeamPlace {
-    uint32_t src, sc, dst0, dst1;           // offsets in a stage
+    uint32_t src, sc, dst0, dst1;           // offsets in a raw stage, and in an operand tile
     __device__ TeamPlace(int thread, int scale_offset, uint32_t codes_at, uint32_t scales_at, uint32_t x_at)
     {
         const int c4 = thread & 3, atom = (thread >> 3) & 1, u = thread >> 4;
@@ -72,7 +72,7 @@ struct TeamPlace {
         dst1 = x_at + (uint32_t)(atom * (64 * 128) + t * 128 + (((2 * c4 + 1) ^ x) << 4));
     }
 };
-__device__ __forceinline__ void transform_stage(uint32_t at, const TeamPlace &p)
+__device__ __forceinline__ void transform_stage(uint32_t at, uint32_t to, const TeamPlace &p)
 {
     uint32_t w[4][4], code[4];
 #pragma unroll
@@ -86,8 +86,8 @@ __device__ __forceinline__ void transform_stage(uint32_t at, const TeamPlace &p)
         uint32_t x[8];
 #pragma unroll
         for (int q = 0; q < 4; ++q) codes_to_bf16(w[j][q], scale, x[2 * q], x[2 * q + 1]);
-        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" :: "r"(at + p.dst0 + (uint32_t)(j * 16 * 128)), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
-        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" :: "r"(at + p.dst1 + (uint32_t)(j * 16 * 128)), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]) : "memory");
+        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" :: "r"(to + p.dst0 + (uint32_t)(j * 16 * 128)), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
+        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" :: "r"(to + p.dst1 + (uint32_t)(j * 16 * 128)), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]) : "memory");
     }
 }
 
@@ -163,17 +163,36 @@ constexpr int kWgBN = 128;
 constexpr int kWgWorkers = 8;
 constexpr int kWgThreads = 32 * (3 + kWgWorkers);
 constexpr int kWgOwn = kWgBN / 2;                                   // columns of a worker thread's row
-constexpr int kWgRaw = 2 * kWgBox;                                  // dy: two boxes
-constexpr int kWgCodes = kWgRaw, kWgScales = kWgCodes + kWgTokens * kWgBN, kWgX = kWgScales + kWgTokens * 16;
-constexpr int kWgStage = kWgX + 2 * kWgBox;                         // 41 KB
-constexpr int kWgStages = 5;
-static_assert(kWgX % 1024 == 0 && kWgStage % 1024 == 0, "operand tiles start on 1024-byte boundaries");
-static_assert(kWgStages * kWgStage >= (128 + 8) * kWgBN * 4 && kWgStages <= kMaxStages, "the ring has room for a tile of partial sums");
+constexpr int kWgCodes = 2 * kWgBox, kWgScales = kWgCodes + kWgTokens * kWgBN;      // in a raw stage, behind two boxes of dy
+// Two rings: what TMA brings, and X in bf16.  One ring whose stages had room for both held five of them; a raw stage is in flight for
+// about a microsecond and in transformation for another, and only the second needs the room for X.
+constexpr int kWgStage = kWgScales + kWgTokens * 16;                // 25 KB
+constexpr int kWgStages = 7, kWgXStage = 2 * kWgBox, kWgXStages = 3;
+constexpr int kWgRings = kWgStages * kWgStage + kWgXStages * kWgXStage;
+static_assert(kWgStage % 1024 == 0, "operand tiles start on 1024-byte boundaries");
+static_assert(kWgRings >= (128 + 8) * kWgBN * 4 && kWgStages <= kMaxStages, "the rings have room for a tile of partial sums");
 
-struct WgradSmall : MxCta {
+// The barriers of the weight gradients' kernels: those of MxBars, of the raw stages, and of free X stages.
+struct WgradBars {
+    MxBars m;
+    uint64_t raw[kMaxStages], x_empty[kWgXStages];
+};
+struct WgradCta : MxCta {
+    __device__ uint32_t raw_bar(int s) const { return bars + (uint32_t)sizeof(MxBars) + (uint32_t)s * 8u; }
+    __device__ uint32_t x_empty_bar(int q) const { return raw_bar(kMaxStages + q); }
+    __device__ uint32_t x_stage(int q) const { return smem + (uint32_t)(kWgStages * kWgStage + q * kWgXStage); }
+};
+// Position in a ring of N stages, and the parity of its phase.
+template <int N>
+struct RingAt {
+    int s = 0;
+    uint32_t ph = 0;
+    __device__ void next() { if (++s == N) { s = 0; ph ^= 1u; } }
+};
+
+struct WgradSmall : WgradCta {
     int64_t n0, k0;
     float *dw;
-    __device__ uint32_t raw_bar(int s) const { return bars + (uint32_t)sizeof(MxBars) + (uint32_t)s * 8u; }
     int first, cols, groups, own, own_valid;
 
     // Two producers: dy, on the full barriers; codes and scales, on the raw ones.  (One thread takes over 0.4 us to issue all
@@ -189,7 +208,7 @@ struct WgradSmall : MxCta {
                 if (it >= S && !mbar_wait(empty_bar(s), ph, abort_flag, g.status, g.wait_limit)) break;
                 const uint32_t bar = DY ? full_bar(s) : raw_bar(s), at = smem + (uint32_t)(s * kWgStage);
                 const int m = (first + it) * kWgTokens;
-                mbar_expect_tx(bar, DY ? kWgCodes : kWgX - kWgCodes);
+                mbar_expect_tx(bar, DY ? kWgCodes : kWgStage - kWgCodes);
                 if (DY) {
                     tma_load_2d(at, &map_a, bar, (int)n0, m);
                     tma_load_2d(at + kWgBox, &map_a, bar, (int)n0 + 64, m);
@@ -211,27 +230,27 @@ struct WgradSmall : MxCta {
     {
         const uint32_t elected = elect_one();
         constexpr uint32_t id = make_idesc_bf16_mn(kWgBN, 128);
-        int s = 0, c = 0;
-        uint32_t ph = 0;
+        RingAt<kWgStages> raw;
+        RingAt<kWgXStages> x;
+        int c = 0;
         for (int it = 0; it < steps; ++it) {
             const int in = it & (kWgChunkSteps - 1);
             if (in == 0 && c >= 2) mbar_wait(freed_bar(c & 1), (uint32_t)((c >> 1) - 1) & 1u, abort_flag, g.status, g.wait_limit);
-            mbar_wait(full_bar(s), ph, abort_flag, g.status, g.wait_limit);
-            mbar_wait(xf_bar(s), ph, abort_flag, g.status, g.wait_limit);
+            mbar_wait(full_bar(raw.s), raw.ph, abort_flag, g.status, g.wait_limit);
+            mbar_wait(xf_bar(x.s), x.ph, abort_flag, g.status, g.wait_limit);
             tc_fence_after();
             const bool chunk_ends = in == kWgChunkSteps - 1 || it == steps - 1;
-            if (elected) {
-                const uint32_t at = smem + (uint32_t)(s * kWgStage), d = tmem + (uint32_t)((c & 1) * kWgBN);
-                const uint64_t adesc = mn_major_desc(at, kWgBox), bdesc = mn_major_desc(at + kWgX, kWgBox);
+            const uint32_t at = smem + (uint32_t)(raw.s * kWgStage), d = tmem + (uint32_t)((c & 1) * kWgBN);
+            const uint64_t adesc = mn_major_desc(at, kWgBox), bdesc = mn_major_desc(x_stage(x.s), kWgBox);
 #pragma unroll
-                for (int k = 0; k < kWgTokens / 16; ++k)
-                    tc_mma_bf16(d, adesc + (uint64_t)(k * 128), bdesc + (uint64_t)(k * 128), id, (in > 0 || k > 0) ? 1u : 0u);
-                tc_commit(empty_bar(s));
-                if (chunk_ends) tc_commit(acc_bar(c & 1));
-            }
-            __syncwarp();
+            for (int k = 0; k < kWgTokens / 16; ++k)
+                tc_mma_bf16(d, adesc + (uint64_t)(k * 128), bdesc + (uint64_t)(k * 128), id, (in > 0 || k > 0) ? 1u : 0u, elected);
+            tc_commit_if(empty_bar(raw.s), elected);
+            tc_commit_if(x_empty_bar(x.s), elected);
+            if (chunk_ends) tc_commit_if(acc_bar(c & 1), elected);
             if (chunk_ends) ++c;
-            if (++s == S) { s = 0; ph ^= 1u; }
+            raw.next();
+            x.next();
         }
         // every MMA has retired before the warp goes on
         mbar_wait(acc_bar((c - 1) & 1), (uint32_t)((c - 1) >> 1) & 1u, abort_flag, g.status, g.wait_limit, true);
@@ -260,20 +279,23 @@ struct WgradSmall : MxCta {
     {
         // a team of four warps takes every other stage: one's barriers and loads run beside the other's arithmetic
         const int team = (warp - 2) >> 2;
-        const TeamPlace place((threadIdx.x - 64) & 127, (int)(k0 / 32) & 15, kWgCodes, kWgScales, kWgX);
+        const TeamPlace place((threadIdx.x - 64) & 127, (int)(k0 / 32) & 15, kWgCodes, kWgScales, 0);
 #pragma unroll
         for (int j = 0; j < kWgOwn; ++j) sum[j] = 0.0f;
-        int s = 0, c = 0;
-        uint32_t ph = 0;
+        RingAt<kWgStages> raw;
+        RingAt<kWgXStages> x;
+        int c = 0;
         for (int it = 0; it < steps; ++it) {
             if ((it & 1) == team) {
-                mbar_wait(raw_bar(s), ph, abort_flag, g.status, g.wait_limit);
-                transform_stage(smem + (uint32_t)(s * kWgStage), place);
+                mbar_wait(raw_bar(raw.s), raw.ph, abort_flag, g.status, g.wait_limit);
+                if (it >= kWgXStages) mbar_wait(x_empty_bar(x.s), x.ph ^ 1u, abort_flag, g.status, g.wait_limit);
+                transform_stage(smem + (uint32_t)(raw.s * kWgStage), x_stage(x.s), place);
                 fence_proxy_async_smem();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(xf_bar(s));
+                if (lane == 0) mbar_arrive(xf_bar(x.s));
             }
-            if (++s == S) { s = 0; ph ^= 1u; }
+            raw.next();
+            x.next();
             if ((it & (kWgChunkSteps - 1)) == kWgChunkSteps - 1 && it < steps - 1) {
                 if (c > 0) add_chunk(g, c - 1, sum);
                 ++c;
@@ -340,7 +362,7 @@ sparq_wgrad_small_kernel(const __grid_constant__ CUtensorMap map_dy, const __gri
                          const __grid_constant__ CUtensorMap map_scales, const WgradArgs g)
 {
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) struct { MxBars bars; uint64_t raw[kMaxStages]; } room;
+    __shared__ __align__(8) WgradBars room;
     __shared__ uint32_t tmem_base_slot;
     __shared__ uint32_t abort_word;
 
@@ -376,8 +398,11 @@ sparq_wgrad_small_kernel(const __grid_constant__ CUtensorMap map_dy, const __gri
             for (int s = 0; s < c.S; ++s) {
                 mbar_init(c.full_bar(s), 1);
                 mbar_init(c.raw_bar(s), 1);
-                mbar_init(c.xf_bar(s), 4);
                 mbar_init(c.empty_bar(s), 1);
+            }
+            for (int q = 0; q < kWgXStages; ++q) {
+                mbar_init(c.xf_bar(q), 4);
+                mbar_init(c.x_empty_bar(q), 1);
             }
             for (int b = 0; b < 2; ++b) {
                 mbar_init(c.acc_bar(b), 1);
@@ -439,7 +464,7 @@ constexpr int kWgFirstWorker = 4;                // whole groups of four warps, 
 constexpr int kWgPairThreads = 32 * (kWgFirstWorker + kWgWorkers);
 
 constexpr int kWgStages16 = 7;
-__host__ __device__ constexpr int wgrad_smem(bool x16) { return 1024 + (x16 ? kWgStages16 * 4 * kWgBox : kWgStages * kWgStage); }
+__host__ __device__ constexpr int wgrad_smem(bool x16) { return 1024 + (x16 ? kWgStages16 * 4 * kWgBox : kWgRings); }
 
 struct WgradPairArgs {
     WgradArgs g;
@@ -465,10 +490,9 @@ __device__ __forceinline__ void wgrad_tile(const WgradPairArgs &p, int t, int &p
 // full: dy of both CTAs, in the leader; raw: codes and scales of this CTA; xf: transformed by both CTAs' workers,
 // in the leader; empty: the MMAs that read the stage have retired; acc, freed: as above.
 template <bool X16>
-struct WgradPair : MxCta {
-    static constexpr int kXAt = X16 ? 2 * kWgBox : kWgX, kStage = kXAt + 2 * kWgBox, kStages = X16 ? kWgStages16 : kWgStages;
+struct WgradPair : WgradCta {
+    static constexpr int kXAt = 2 * kWgBox, kStage = X16 ? kXAt + kWgXStage : kWgStage, kStages = X16 ? kWgStages16 : kWgStages;
     int tiles, pair;
-    __device__ uint32_t raw_bar(int s) const { return bars + (uint32_t)sizeof(MxBars) + (uint32_t)s * 8u; }
 
     template <bool DY>
     __device__ void produce(const CUtensorMap &map_a, const CUtensorMap &map_b, const WgradPairArgs &p) const
@@ -498,7 +522,7 @@ struct WgradPair : MxCta {
                         tma_load_pair_2d(at + kXAt, &map_a, bar, k, m);
                         tma_load_pair_2d(at + kXAt + kWgBox, &map_a, bar, k + 64, m);
                     } else {
-                        mbar_expect_tx(raw_bar(s), kWgX - kWgCodes);
+                        mbar_expect_tx(raw_bar(s), kWgStage - kWgCodes);
                         tma_load_2d(at + kWgCodes, &map_a, raw_bar(s), k, m);
                         tma_load_2d(at + kWgScales, &map_b, raw_bar(s), sc, m);
                     }
@@ -527,29 +551,29 @@ struct WgradPair : MxCta {
             const WgradArgs &g = p.g;
             const uint32_t elected = elect_one();
             constexpr uint32_t id = make_idesc_bf16_mn(kWgTile, 256);
-            int s = 0, c = 0;
-            uint32_t ph = 0;
+            RingAt<kStages> raw;
+            RingAt<kWgXStages> x;
+            int c = 0;
             for (int t = pair; t < tiles; t += p.pairs) {
                 const int part = g.part + t / (p.n_tiles * p.k_tiles), steps_of = part_begin(g, part + 1) - part_begin(g, part);
                 for (int b = 0; b < steps_of; ++b) {
                     const int in = b & (kWgChunkSteps - 1);
                     if (in == 0 && c >= 2) mbar_wait(freed_bar(c & 1), (uint32_t)((c >> 1) - 1) & 1u, abort_flag, g.status, g.wait_limit);
-                    mbar_wait(full_bar(s), ph, abort_flag, g.status, g.wait_limit);
-                    if (!X16) mbar_wait(xf_bar(s), ph, abort_flag, g.status, g.wait_limit);
+                    mbar_wait(full_bar(raw.s), raw.ph, abort_flag, g.status, g.wait_limit);
+                    if (!X16) mbar_wait(xf_bar(x.s), x.ph, abort_flag, g.status, g.wait_limit);
                     tc_fence_after();
                     const bool chunk_ends = in == kWgChunkSteps - 1 || b == steps_of - 1;
-                    if (elected) {
-                        const uint32_t at = smem + (uint32_t)(s * kStage), d = tmem + (uint32_t)((c & 1) * kWgTile);
-                        const uint64_t adesc = mn_major_desc(at, kWgBox), bdesc = mn_major_desc(at + kXAt, kWgBox);
+                    const uint32_t at = smem + (uint32_t)(raw.s * kStage), d = tmem + (uint32_t)((c & 1) * kWgTile);
+                    const uint64_t adesc = mn_major_desc(at, kWgBox), bdesc = mn_major_desc(X16 ? at + kXAt : x_stage(x.s), kWgBox);
 #pragma unroll
-                        for (int k = 0; k < kWgTokens / 16; ++k)
-                            tc_mma_bf16_pair(d, adesc + (uint64_t)(k * 128), bdesc + (uint64_t)(k * 128), id, (in > 0 || k > 0) ? 1u : 0u);
-                        tc_commit_pair(empty_bar(s));
-                        if (chunk_ends) tc_commit_pair(acc_bar(c & 1));
-                    }
-                    __syncwarp();
+                    for (int k = 0; k < kWgTokens / 16; ++k)
+                        tc_mma_bf16_pair(d, adesc + (uint64_t)(k * 128), bdesc + (uint64_t)(k * 128), id, (in > 0 || k > 0) ? 1u : 0u, elected);
+                    tc_commit_pair(empty_bar(raw.s), elected);
+                    if (!X16) tc_commit_pair(x_empty_bar(x.s), elected);
+                    if (chunk_ends) tc_commit_pair(acc_bar(c & 1), elected);
                     if (chunk_ends) ++c;
-                    if (++s == kStages) { s = 0; ph ^= 1u; }
+                    raw.next();
+                    x.next();
                 }
             }
             // every MMA has retired before the warp goes on
@@ -587,26 +611,32 @@ struct WgradPair : MxCta {
         // a team of four warps takes every other stage: one's barriers and loads run beside the other's arithmetic
         const int team = (warp - kWgFirstWorker) >> 2;
         const uint32_t leader_xf = map_to_rank(xf_bar(0), 0), leader_freed = map_to_rank(freed_bar(0), 0);
-        int s = 0, c = 0, stage = 0;
-        uint32_t ph = 0;
+        RingAt<kStages> raw;
+        RingAt<kWgXStages> x;
+        int c = 0, stage = 0;
         for (int t = pair; t < tiles; t += p.pairs) {
             int part, nt, kt;
             wgrad_tile(p, t, part, nt, kt);
             const int steps_of = part_begin(g, part + 1) - part_begin(g, part);
-            const TeamPlace place(threadIdx.x & 127, ((kt * kWgTile + rank * 128) / 32) & 15, kWgCodes, kWgScales, kWgX);
+            const TeamPlace place(threadIdx.x & 127, ((kt * kWgTile + rank * 128) / 32) & 15, kWgCodes, kWgScales, 0);
             float sum[kWgPairOwn];
 #pragma unroll
             for (int j = 0; j < kWgPairOwn; ++j) sum[j] = 0.0f;
             const int c_first = c;
             for (int b = 0; b < steps_of; ++b) {
-                if (!X16 && (stage++ & 1) == team) {
-                    mbar_wait(raw_bar(s), ph, abort_flag, g.status, g.wait_limit);
-                    transform_stage(smem + (uint32_t)(s * kStage), place);
-                    fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_remote(leader_xf + 8u * (uint32_t)s);
+                if (!X16) {
+                    if ((stage & 1) == team) {
+                        mbar_wait(raw_bar(raw.s), raw.ph, abort_flag, g.status, g.wait_limit);
+                        if (stage >= kWgXStages) mbar_wait(x_empty_bar(x.s), x.ph ^ 1u, abort_flag, g.status, g.wait_limit);
+                        transform_stage(smem + (uint32_t)(raw.s * kStage), x_stage(x.s), place);
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_remote(leader_xf + 8u * (uint32_t)x.s);
+                    }
+                    ++stage;
+                    raw.next();
+                    x.next();
                 }
-                if (!X16 && ++s == kStages) { s = 0; ph ^= 1u; }
                 if ((b & (kWgChunkSteps - 1)) == kWgChunkSteps - 1 && b < steps_of - 1) {
                     if (c > c_first) add_chunk(g, c - 1, leader_freed, sum);
                     ++c;
@@ -626,7 +656,7 @@ sparq_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_cons
                    const __grid_constant__ CUtensorMap map_scales, const WgradPairArgs p)
 {
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) struct { MxBars bars; uint64_t raw[kMaxStages]; } room;
+    __shared__ __align__(8) WgradBars room;
     __shared__ uint32_t tmem_base_slot;
     __shared__ uint32_t abort_word;
 
@@ -648,8 +678,11 @@ sparq_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_cons
             for (int s = 0; s < Cta::kStages; ++s) {
                 mbar_init(c.full_bar(s), 1);
                 mbar_init(c.raw_bar(s), 1);
-                mbar_init(c.xf_bar(s), 2 * 4);         // a team of each CTA
                 mbar_init(c.empty_bar(s), 1);
+            }
+            for (int q = 0; q < kWgXStages; ++q) {
+                mbar_init(c.xf_bar(q), 2 * 4);         // a team of each CTA
+                mbar_init(c.x_empty_bar(q), 1);
             }
             for (int b = 0; b < 2; ++b) {
                 mbar_init(c.acc_bar(b), 1);
