@@ -88,6 +88,43 @@ __device__ __forceinline__ void tma_load_bytes(uint32_t dst, const void *src, ui
 
 __host__ __device__ constexpr int tmem_columns(int want) { return want <= 32 ? 32 : want <= 64 ? 64 : want <= 128 ? 128 : want <= 256 ? 256 : 512; }
 
+// mbar_wait of a converged warp through one of its lanes.  Every lane's own look at a barrier, complete or not, takes its turn: about
+// 130 cycles for 32 of them, which in a loop of a few hundred cycles is what the loop takes.  The lanes decide together, by votes, so
+// that the warp stays converged for the instructions behind the wait that need it to be.
+__device__ __forceinline__ bool mbar_try_wait_of(uint32_t mine, uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.b32 q, %3, 0;\n\t"
+        "setp.ne.b32 p, 0, 0;\n\t"
+        "@q mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(bar), "r"(parity), "r"(mine) : "memory");
+    return __any_sync(0xFFFFFFFFu, ok);
+}
+__device__ __forceinline__ void mbar_wait_warp(uint32_t mine, uint32_t bar, uint32_t parity, volatile uint32_t *abort_flag, unsigned int *status,
+                                               long long limit_cycles)
+{
+    if (mbar_try_wait_of(mine, bar, parity)) return;
+    if (__any_sync(0xFFFFFFFFu, *abort_flag != 0u)) return;
+    const long long t0 = clock64();
+    for (uint32_t it = 1;; ++it) {
+        if (mbar_try_wait_of(mine, bar, parity)) return;
+        if ((it & 0x3Fu) == 0) {
+            if (__any_sync(0xFFFFFFFFu, *abort_flag != 0u)) return;
+            if (__any_sync(0xFFFFFFFFu, clock64() - t0 > limit_cycles)) {
+                if (mine) {
+                    *abort_flag = 1u;
+                    atomicOr(status, 1u);
+                }
+                __syncwarp();
+                return;
+            }
+        }
+    }
+}
+
 // ---- CTA pairs (cta_group::2): one MMA over the operands and tensor memory of both ---------------------
 // The even CTA of the pair (the leader) issues; A's and D's rows and B's rows are halved between the two.
 

@@ -104,9 +104,9 @@ struct Mxf4Pair : MxCta {
             uint32_t ph = 0;
             for (int t = pair; t < tiles; t += p.pairs, ++i) {
                 const uint32_t d = tmem + (i & 1) * kPairSecond;
-                if (i > 0) mbar_wait(freed_bar(0), (uint32_t)(i - 1) & 1u, abort_flag, g.status, g.wait_limit);
+                if (i > 0) mbar_wait_warp(elected, freed_bar(0), (uint32_t)(i - 1) & 1u, abort_flag, g.status, g.wait_limit);
                 for (int kb = 0; kb < g.k_blocks; ++kb) {
-                    mbar_wait(full_bar(s), ph, abort_flag, g.status, g.wait_limit);
+                    mbar_wait_warp(elected, full_bar(s), ph, abort_flag, g.status, g.wait_limit);
                     tc_fence_after();
                     const uint32_t at = smem + (uint32_t)(s * kRoom), sf = at + kScalesAt, ta = tmem + kPairScales, tb = ta + 4 * T;
                     const uint64_t adesc = make_smem_desc<kMxBK>(at), bdesc = make_smem_desc<kMxBK>(at + kHalf);

@@ -213,7 +213,7 @@ struct Mxf4Small : MxCta {
         int s = 0;
         uint32_t ph = 0;
         for (int it = 0; it < steps; ++it) {
-            mbar_wait(full_bar(s), ph, abort_flag, g.status, g.wait_limit);
+            mbar_wait_warp(elected, full_bar(s), ph, abort_flag, g.status, g.wait_limit);
             tc_fence_after();
             const uint32_t at = smem + (uint32_t)(s * kStage), sf = at + kScalesAt;
             const int mmas = g.k_mmas - (kb_first + it) * kMxSteps;

@@ -127,9 +127,11 @@ extern "C" int sparq_wgrad_mx8(const void *dy, int64_t lddy, const int8_t *codes
     // Memory for X in bf16 and for the parts' sums: the caller's, else scratch.  Without any (a stream that is being captured) X is expanded
     // stage by stage and the parts add to dw one launch after the other: the same sums in the same order.
     CUtensorMap map_x;
-    void *const own = !workspace && need.x ? workspace_alloc(need.x, st) : nullptr, *const own_sums = !workspace && need.sums ? workspace_alloc(need.sums, st) : nullptr;
-    void *const x = workspace && need.x ? workspace : own;
-    float *const sums = (float *)(workspace && need.sums ? (uint8_t *)workspace + need.x : own_sums);
+    const size_t bytes = need.x + need.sums;
+    void *const own = !workspace && bytes ? workspace_alloc(bytes, st) : nullptr;
+    uint8_t *const room = (uint8_t *)(workspace ? workspace : own);
+    void *const x = room && need.x ? room : nullptr;
+    float *const sums = room && need.sums ? (float *)(room + need.x) : nullptr;
     rc = SPARQ_OK;
     if (x) {
         rc = sparq_dequantize_mx(codes, scales, M, K, SPARQ_MXINT8, nullptr, x, SPARQ_DTYPE_BF16, pitch, stream);
@@ -165,7 +167,6 @@ extern "C" int sparq_wgrad_mx8(const void *dy, int64_t lddy, const int8_t *codes
                                                 g.parts, (int)(accumulate != 0), dw);
         if (e != cudaSuccess) rc = cuda_error(e, "wgrad_add_parts_kernel launch");
     }
-    workspace_free(own_sums, st);
     workspace_free(own, st);
     return rc;
 }

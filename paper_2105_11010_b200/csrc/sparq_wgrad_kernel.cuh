@@ -235,9 +235,9 @@ struct WgradSmall : WgradCta {
         int c = 0;
         for (int it = 0; it < steps; ++it) {
             const int in = it & (kWgChunkSteps - 1);
-            if (in == 0 && c >= 2) mbar_wait(freed_bar(c & 1), (uint32_t)((c >> 1) - 1) & 1u, abort_flag, g.status, g.wait_limit);
-            mbar_wait(full_bar(raw.s), raw.ph, abort_flag, g.status, g.wait_limit);
-            mbar_wait(xf_bar(x.s), x.ph, abort_flag, g.status, g.wait_limit);
+            if (in == 0 && c >= 2) mbar_wait_warp(elected, freed_bar(c & 1), (uint32_t)((c >> 1) - 1) & 1u, abort_flag, g.status, g.wait_limit);
+            mbar_wait_warp(elected, full_bar(raw.s), raw.ph, abort_flag, g.status, g.wait_limit);
+            mbar_wait_warp(elected, xf_bar(x.s), x.ph, abort_flag, g.status, g.wait_limit);
             tc_fence_after();
             const bool chunk_ends = in == kWgChunkSteps - 1 || it == steps - 1;
             const uint32_t at = smem + (uint32_t)(raw.s * kWgStage), d = tmem + (uint32_t)((c & 1) * kWgBN);
@@ -287,8 +287,8 @@ struct WgradSmall : WgradCta {
         int c = 0;
         for (int it = 0; it < steps; ++it) {
             if ((it & 1) == team) {
-                mbar_wait(raw_bar(raw.s), raw.ph, abort_flag, g.status, g.wait_limit);
-                if (it >= kWgXStages) mbar_wait(x_empty_bar(x.s), x.ph ^ 1u, abort_flag, g.status, g.wait_limit);
+                mbar_wait_warp(lane == 0 ? 1u : 0u, raw_bar(raw.s), raw.ph, abort_flag, g.status, g.wait_limit);
+                if (it >= kWgXStages) mbar_wait_warp(lane == 0 ? 1u : 0u, x_empty_bar(x.s), x.ph ^ 1u, abort_flag, g.status, g.wait_limit);
                 transform_stage(smem + (uint32_t)(raw.s * kWgStage), x_stage(x.s), place);
                 fence_proxy_async_smem();
                 __syncwarp();
@@ -558,9 +558,9 @@ struct WgradPair : WgradCta {
                 const int part = g.part + t / (p.n_tiles * p.k_tiles), steps_of = part_begin(g, part + 1) - part_begin(g, part);
                 for (int b = 0; b < steps_of; ++b) {
                     const int in = b & (kWgChunkSteps - 1);
-                    if (in == 0 && c >= 2) mbar_wait(freed_bar(c & 1), (uint32_t)((c >> 1) - 1) & 1u, abort_flag, g.status, g.wait_limit);
-                    mbar_wait(full_bar(raw.s), raw.ph, abort_flag, g.status, g.wait_limit);
-                    if (!X16) mbar_wait(xf_bar(x.s), x.ph, abort_flag, g.status, g.wait_limit);
+                    if (in == 0 && c >= 2) mbar_wait_warp(elected, freed_bar(c & 1), (uint32_t)((c >> 1) - 1) & 1u, abort_flag, g.status, g.wait_limit);
+                    mbar_wait_warp(elected, full_bar(raw.s), raw.ph, abort_flag, g.status, g.wait_limit);
+                    if (!X16) mbar_wait_warp(elected, xf_bar(x.s), x.ph, abort_flag, g.status, g.wait_limit);
                     tc_fence_after();
                     const bool chunk_ends = in == kWgChunkSteps - 1 || b == steps_of - 1;
                     const uint32_t at = smem + (uint32_t)(raw.s * kStage), d = tmem + (uint32_t)((c & 1) * kWgTile);
@@ -626,8 +626,8 @@ struct WgradPair : WgradCta {
             for (int b = 0; b < steps_of; ++b) {
                 if (!X16) {
                     if ((stage & 1) == team) {
-                        mbar_wait(raw_bar(raw.s), raw.ph, abort_flag, g.status, g.wait_limit);
-                        if (stage >= kWgXStages) mbar_wait(x_empty_bar(x.s), x.ph ^ 1u, abort_flag, g.status, g.wait_limit);
+                        mbar_wait_warp(lane == 0 ? 1u : 0u, raw_bar(raw.s), raw.ph, abort_flag, g.status, g.wait_limit);
+                        if (stage >= kWgXStages) mbar_wait_warp(lane == 0 ? 1u : 0u, x_empty_bar(x.s), x.ph ^ 1u, abort_flag, g.status, g.wait_limit);
                         transform_stage(smem + (uint32_t)(raw.s * kStage), x_stage(x.s), place);
                         fence_proxy_async_smem();
                         __syncwarp();
