@@ -9,6 +9,7 @@
 // Every function takes its arguments by position in the order of the wrappers in _binding.py,
 // which own the keyword names and defaults, and returns the C ABI's status.
 #include <torch/csrc/autograd/python_variable.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 
 #include "sparq.h"
@@ -431,11 +432,19 @@ SPARQ_PY(py_gemm_sparse24)
 
 // ---- microscaled formats ----
 
+// The work is launched on the current device: a tensor of another one is refused.
+const Tensor *here(const Tensor *t, const char *name)
+{
+    if (t && t->is_cuda() && t->get_device() != c10::cuda::current_device()) fail("%s is on another device than the current one", name);
+    return t;
+}
+
 // A matrix of float32 / bfloat16 whose rows are contiguous; its leading dimension.
 const void *float_rows(const Tensor &t, const char *name, int *dtype, int64_t *ld)
 {
     const bool bf16 = t.scalar_type() == at::kBFloat16;
     if (!t.is_cuda() || !(bf16 || t.scalar_type() == at::kFloat)) fail("%s must be a CUDA tensor of float32 or bfloat16", name);
+    here(&t, name);
     if (t.dim() != 2) fail("%s must be a matrix", name);
     if (t.size(1) > 1 && t.stride(1) != 1) fail("%s must have contiguous rows", name);
     *dtype = bf16 ? SPARQ_DTYPE_BF16 : SPARQ_DTYPE_F32;
@@ -458,6 +467,7 @@ const void *float_rows_like(const Tensor &t, const char *name, const Tensor &as,
 void *mx_codes(const Tensor *t, const char *name, int format, int64_t rows, int64_t cols)
 {
     if (!t) return nullptr;
+    here(t, name);
     const int64_t want = sparq_mx_code_bytes(format, rows, cols);
     if (want >= 0 && t->numel() < want) fail("%s is smaller than sparq_mx_code_bytes says", name);
     return format == SPARQ_MXINT8 ? (void *)data<int8_t>(t, at::kChar, name) : (void *)data<uint8_t>(t, at::kByte, name);
@@ -465,6 +475,7 @@ void *mx_codes(const Tensor *t, const char *name, int format, int64_t rows, int6
 uint8_t *mx_scales(const Tensor *t, const char *name, int format, int64_t rows, int64_t cols)
 {
     if (!t) return nullptr;
+    here(t, name);
     const int64_t want = sparq_mx_scale_bytes(format, rows, cols);
     if (want >= 0 && t->numel() < want) fail("%s is smaller than sparq_mx_scale_bytes says", name);
     return data<uint8_t>(t, at::kByte, name);
@@ -472,7 +483,7 @@ uint8_t *mx_scales(const Tensor *t, const char *name, int format, int64_t rows, 
 float *one_float(const Tensor *t, const char *name)
 {
     if (t && t->numel() < 1) fail("%s is empty", name);
-    return data<float>(t, at::kFloat, name);
+    return data<float>(here(t, name), at::kFloat, name);
 }
 
 // (values, format, codes, scales, max_dev, stream); `values` is the input or, decoding, the output
@@ -517,13 +528,13 @@ SPARQ_PY(py_gemm_mxf4)
         e.b_max = one_float(a.opt("b_max"), "b_max");
         const Tensor *bias = a.opt("bias");
         if (bias && bias->numel() < N) fail("%s has fewer than N elements", "bias");
-        e.bias = data<float>(bias, at::kFloat, "bias");
+        e.bias = data<float>(here(bias, "bias"), at::kFloat, "bias");
         e.relu = a.truth();
         const Tensor *f32 = a.opt("f32_out"), *bf16 = a.opt("bf16_out");
         if (f32 && f32->numel() < M * N) fail("%s has fewer than M*N elements", "f32_out");
         if (bf16 && bf16->numel() < M * N) fail("%s has fewer than M*N elements", "bf16_out");
-        e.f32_out = data<float>(f32, at::kFloat, "f32_out");
-        e.bf16_out = data<void>(bf16, at::kBFloat16, "bf16_out");
+        e.f32_out = data<float>(here(f32, "f32_out"), at::kFloat, "f32_out");
+        e.bf16_out = data<void>(here(bf16, "bf16_out"), at::kBFloat16, "bf16_out");
         const bool four = format == SPARQ_MXFP4 || format == SPARQ_NVFP4;      // the library refuses others
         const void *pa = four ? mx_codes(&A, "A", format, M, K) : data<void>(&A, at::kByte, "A");
         const void *pb = four ? mx_codes(&B, "B", format, N, K) : data<void>(&B, at::kByte, "B");
@@ -594,10 +605,10 @@ SPARQ_PY(py_wgrad_mx8)
         const int64_t M = dy.size(0), N = dy.size(1), K = dw.size(1);
         const int8_t *pc = (int8_t *)mx_codes(&c, "codes", SPARQ_MXINT8, M, K);
         const uint8_t *ps = mx_scales(&s, "scales", SPARQ_MXINT8, M, K);
-        float *pdw = data<float>(&dw, at::kFloat, "dw");
+        float *pdw = data<float>(here(&dw, "dw"), at::kFloat, "dw");
         const int accumulate = a.truth();
         const Tensor *ws = a.opt("workspace");
-        uint8_t *pws = data<uint8_t>(ws, at::kByte, "workspace");
+        uint8_t *pws = data<uint8_t>(here(ws, "workspace"), at::kByte, "workspace");
         const size_t ws_bytes = ws ? (size_t)ws->numel() : 0;
         void *st = a.stream();
         return call([&] { return sparq_wgrad_mx8(pdy, ld, pc, ps, M, N, K, accumulate, pdw, pws, ws_bytes, st); });

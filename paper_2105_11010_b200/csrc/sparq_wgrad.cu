@@ -156,7 +156,7 @@ extern "C" int sparq_wgrad_mx8(const void *dy, int64_t lddy, const int8_t *codes
                   : launch_wgrad(sparq_wgrad_kernel<false>, set_q, 2 * p.pairs, 2, kWgPairThreads, wgrad_smem(false), st, map_dy, map_codes, map_scales, p);
         } else {
             static bool set[64] = {};
-            e = launch_wgrad(sparq_wgrad_small_kernel, set, (int)(form.tiles * g.count * g.split), g.split, kWgThreads, wgrad_smem(false), st,
+            e = launch_wgrad(sparq_wgrad_small_kernel, set, (int)(form.tiles * g.count * g.split), g.split, kWgThreads, 1024 + WgradSmall::kRings, st,
                              map_dy, map_codes, map_scales, g);
         }
         if (e != cudaSuccess) rc = cuda_error(e, "weight gradient kernel launch");

@@ -156,31 +156,31 @@ __device__ __forceinline__ void wgrad_put_row(float *out, const float (&sum)[C],
 // Tiles of 128 x 128, a cluster of `split` CTAs on each that take equal runs of tokens: their partial sums go to the CTA that
 // owns a group of four columns through distributed shared memory (the operand ring's, once every CTA of the cluster is
 // done with it), and are added in rank order.
-// Warps: 0 producer of dy, 10 of codes and scales, 1 tensor memory and MMA issue, 2..9 workers: they transform the stages, and after a
-// chunk's last one add up the chunk before (warp w: lane quarter w % 4, half of the columns).
+// Warps: 0 producer of dy, 18 of codes and scales, 1 tensor memory and MMA issue, 2..17 workers: they transform the stages, and after a
+// chunk's last one add up the chunk before (warp w: lane quarter w % 4, a quarter of the columns).
 
 constexpr int kWgBN = 128;
-constexpr int kWgWorkers = 8;
+constexpr int kWgTeams = 4, kWgWorkers = 4 * kWgTeams;
 constexpr int kWgThreads = 32 * (3 + kWgWorkers);
-constexpr int kWgOwn = kWgBN / 2;                                   // columns of a worker thread's row
+constexpr int kWgOwn = kWgBN / kWgTeams;                            // columns of a worker thread's row
 constexpr int kWgCodes = 2 * kWgBox, kWgScales = kWgCodes + kWgTokens * kWgBN;      // in a raw stage, behind two boxes of dy
-// Two rings: what TMA brings, and X in bf16.  One ring whose stages had room for both held five of them; a raw stage is in flight for
-// about a microsecond and in transformation for another, and only the second needs the room for X.
+// Two rings: R stages of what TMA brings, and X stages of X in bf16, which the teams write while the MMAs read another.
 constexpr int kWgStage = kWgScales + kWgTokens * 16;                // 25 KB
-constexpr int kWgStages = 7, kWgXStage = 2 * kWgBox, kWgXStages = 3;
-constexpr int kWgRings = kWgStages * kWgStage + kWgXStages * kWgXStage;
+constexpr int kWgXStage = 2 * kWgBox;
 static_assert(kWgStage % 1024 == 0, "operand tiles start on 1024-byte boundaries");
-static_assert(kWgRings >= (128 + 8) * kWgBN * 4 && kWgStages <= kMaxStages, "the rings have room for a tile of partial sums");
 
 // The barriers of the weight gradients' kernels: those of MxBars, of the raw stages, and of free X stages.
 struct WgradBars {
     MxBars m;
-    uint64_t raw[kMaxStages], x_empty[kWgXStages];
+    uint64_t raw[kMaxStages], x_empty[kMaxStages];
 };
+template <int R, int X>
 struct WgradCta : MxCta {
+    static constexpr int kRaw = R, kX = X, kRings = R * kWgStage + X * kWgXStage;
+    static_assert(R <= kMaxStages && X <= kMaxStages, "a barrier for each stage");
     __device__ uint32_t raw_bar(int s) const { return bars + (uint32_t)sizeof(MxBars) + (uint32_t)s * 8u; }
     __device__ uint32_t x_empty_bar(int q) const { return raw_bar(kMaxStages + q); }
-    __device__ uint32_t x_stage(int q) const { return smem + (uint32_t)(kWgStages * kWgStage + q * kWgXStage); }
+    __device__ uint32_t x_stage(int q) const { return smem + (uint32_t)(R * kWgStage + q * kWgXStage); }
 };
 // Position in a ring of N stages, and the parity of its phase.
 template <int N>
@@ -190,7 +190,8 @@ struct RingAt {
     __device__ void next() { if (++s == N) { s = 0; ph ^= 1u; } }
 };
 
-struct WgradSmall : WgradCta {
+struct WgradSmall : WgradCta<6, 4> {
+    static_assert(kRings >= (128 + 8) * kWgBN * 4, "the rings have room for a tile of partial sums");
     int64_t n0, k0;
     float *dw;
     int first, cols, groups, own, own_valid;
@@ -230,8 +231,8 @@ struct WgradSmall : WgradCta {
     {
         const uint32_t elected = elect_one();
         constexpr uint32_t id = make_idesc_bf16_mn(kWgBN, 128);
-        RingAt<kWgStages> raw;
-        RingAt<kWgXStages> x;
+        RingAt<kRaw> raw;
+        RingAt<kX> x;
         int c = 0;
         for (int it = 0; it < steps; ++it) {
             const int in = it & (kWgChunkSteps - 1);
@@ -277,18 +278,19 @@ struct WgradSmall : WgradCta {
 
     __device__ void work(const WgradArgs &g, float (&sum)[kWgOwn]) const
     {
-        // a team of four warps takes every other stage: one's barriers and loads run beside the other's arithmetic
+        // A team of four warps takes every fourth stage: a stage's chain of barriers, loads, arithmetic and stores is mostly latency, which the
+        // other teams' fill (two teams: 0.51 us a step, of which 0.3 are there without any transform).
         const int team = (warp - 2) >> 2;
         const TeamPlace place((threadIdx.x - 64) & 127, (int)(k0 / 32) & 15, kWgCodes, kWgScales, 0);
 #pragma unroll
         for (int j = 0; j < kWgOwn; ++j) sum[j] = 0.0f;
-        RingAt<kWgStages> raw;
-        RingAt<kWgXStages> x;
+        RingAt<kRaw> raw;
+        RingAt<kX> x;
         int c = 0;
         for (int it = 0; it < steps; ++it) {
-            if ((it & 1) == team) {
+            if (it % kWgTeams == team) {
                 mbar_wait_warp(lane == 0 ? 1u : 0u, raw_bar(raw.s), raw.ph, abort_flag, g.status, g.wait_limit);
-                if (it >= kWgXStages) mbar_wait_warp(lane == 0 ? 1u : 0u, x_empty_bar(x.s), x.ph ^ 1u, abort_flag, g.status, g.wait_limit);
+                if (it >= kX) mbar_wait_warp(lane == 0 ? 1u : 0u, x_empty_bar(x.s), x.ph ^ 1u, abort_flag, g.status, g.wait_limit);
                 transform_stage(smem + (uint32_t)(raw.s * kWgStage), x_stage(x.s), place);
                 fence_proxy_async_smem();
                 __syncwarp();
@@ -341,7 +343,7 @@ struct WgradSmall : WgradCta {
                            __float_as_uint(a[2]), __float_as_uint(a[3]));
         }
         mbar_wait(recv_bar(), 0, abort_flag, g.status, g.wait_limit, true);
-        for (int local = half; local < own_valid; local += 2) {
+        for (int local = half; local < own_valid; local += kWgTeams) {
             float a[4] = {0.0f, 0.0f, 0.0f, 0.0f};
             for (uint32_t q = 0; q < split; ++q) {
                 uint4 p;
@@ -369,7 +371,7 @@ sparq_wgrad_small_kernel(const __grid_constant__ CUtensorMap map_dy, const __gri
     WgradSmall c;
     const int warp = c.warp = threadIdx.x >> 5, lane = c.lane = threadIdx.x & 31;
     c.abort_flag = &abort_word;
-    c.S = kWgStages;
+    c.S = WgradSmall::kRaw;
     c.smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
     c.bars = smem_u32(&room);
     const uint32_t split = c.split = (uint32_t)g.split, item = blockIdx.x / split;
@@ -400,7 +402,7 @@ sparq_wgrad_small_kernel(const __grid_constant__ CUtensorMap map_dy, const __gri
                 mbar_init(c.raw_bar(s), 1);
                 mbar_init(c.empty_bar(s), 1);
             }
-            for (int q = 0; q < kWgXStages; ++q) {
+            for (int q = 0; q < WgradSmall::kX; ++q) {
                 mbar_init(c.xf_bar(q), 4);
                 mbar_init(c.x_empty_bar(q), 1);
             }
@@ -458,13 +460,14 @@ sparq_wgrad_small_kernel(const __grid_constant__ CUtensorMap map_dy, const __gri
 // columns of a row in registers.
 
 constexpr int kWgTile = 256;
+constexpr int kWgPairWorkers = 8;
 constexpr int kWgPairOwn = 128;                  // columns of a worker thread's row
 constexpr int kWgCodeWarp = 2;
 constexpr int kWgFirstWorker = 4;                // whole groups of four warps, for setmaxnreg
-constexpr int kWgPairThreads = 32 * (kWgFirstWorker + kWgWorkers);
+constexpr int kWgPairThreads = 32 * (kWgFirstWorker + kWgPairWorkers);
 
 constexpr int kWgStages16 = 7;
-__host__ __device__ constexpr int wgrad_smem(bool x16) { return 1024 + (x16 ? kWgStages16 * 4 * kWgBox : kWgRings); }
+__host__ __device__ constexpr int wgrad_smem(bool x16) { return 1024 + (x16 ? kWgStages16 * 4 * kWgBox : WgradCta<7, 3>::kRings); }
 
 struct WgradPairArgs {
     WgradArgs g;
@@ -490,8 +493,8 @@ __device__ __forceinline__ void wgrad_tile(const WgradPairArgs &p, int t, int &p
 // full: dy of both CTAs, in the leader; raw: codes and scales of this CTA; xf: transformed by both CTAs' workers,
 // in the leader; empty: the MMAs that read the stage have retired; acc, freed: as above.
 template <bool X16>
-struct WgradPair : WgradCta {
-    static constexpr int kXAt = 2 * kWgBox, kStage = X16 ? kXAt + kWgXStage : kWgStage, kStages = X16 ? kWgStages16 : kWgStages;
+struct WgradPair : WgradCta<7, 3> {
+    static constexpr int kXAt = 2 * kWgBox, kStage = X16 ? kXAt + kWgXStage : kWgStage, kStages = X16 ? kWgStages16 : kRaw;
     int tiles, pair;
 
     template <bool DY>
@@ -552,7 +555,7 @@ struct WgradPair : WgradCta {
             const uint32_t elected = elect_one();
             constexpr uint32_t id = make_idesc_bf16_mn(kWgTile, 256);
             RingAt<kStages> raw;
-            RingAt<kWgXStages> x;
+            RingAt<kX> x;
             int c = 0;
             for (int t = pair; t < tiles; t += p.pairs) {
                 const int part = g.part + t / (p.n_tiles * p.k_tiles), steps_of = part_begin(g, part + 1) - part_begin(g, part);
@@ -612,7 +615,7 @@ struct WgradPair : WgradCta {
         const int team = (warp - kWgFirstWorker) >> 2;
         const uint32_t leader_xf = map_to_rank(xf_bar(0), 0), leader_freed = map_to_rank(freed_bar(0), 0);
         RingAt<kStages> raw;
-        RingAt<kWgXStages> x;
+        RingAt<kX> x;
         int c = 0, stage = 0;
         for (int t = pair; t < tiles; t += p.pairs) {
             int part, nt, kt;
@@ -627,7 +630,7 @@ struct WgradPair : WgradCta {
                 if (!X16) {
                     if ((stage & 1) == team) {
                         mbar_wait_warp(lane == 0 ? 1u : 0u, raw_bar(raw.s), raw.ph, abort_flag, g.status, g.wait_limit);
-                        if (stage >= kWgXStages) mbar_wait_warp(lane == 0 ? 1u : 0u, x_empty_bar(x.s), x.ph ^ 1u, abort_flag, g.status, g.wait_limit);
+                        if (stage >= kX) mbar_wait_warp(lane == 0 ? 1u : 0u, x_empty_bar(x.s), x.ph ^ 1u, abort_flag, g.status, g.wait_limit);
                         transform_stage(smem + (uint32_t)(raw.s * kStage), x_stage(x.s), place);
                         fence_proxy_async_smem();
                         __syncwarp();
@@ -680,13 +683,13 @@ sparq_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_cons
                 mbar_init(c.raw_bar(s), 1);
                 mbar_init(c.empty_bar(s), 1);
             }
-            for (int q = 0; q < kWgXStages; ++q) {
+            for (int q = 0; q < Cta::kX; ++q) {
                 mbar_init(c.xf_bar(q), 2 * 4);         // a team of each CTA
                 mbar_init(c.x_empty_bar(q), 1);
             }
             for (int b = 0; b < 2; ++b) {
                 mbar_init(c.acc_bar(b), 1);
-                mbar_init(c.freed_bar(b), 2 * kWgWorkers);
+                mbar_init(c.freed_bar(b), 2 * kWgPairWorkers);
             }
             abort_word = 0;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
