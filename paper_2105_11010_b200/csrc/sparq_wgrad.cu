@@ -39,7 +39,8 @@ WgradForm pick_wgrad(int64_t M, int64_t N, int64_t K, int blocks, int sms)
         if (parts > 1 && (double)parts * (double)N * (double)K * 4.0 > (double)kWorkspaceMaxBytes) break;
         const int b = (blocks + parts - 1) / parts;
         const double join = parts > 1 ? 2.5 + (double)(parts + 1) * (double)N * (double)K * 4.0 / 5.0e6 : 0.0;
-        for (int split = 1; split <= 8 && split <= b; split *= 2) {
+        // (the shorter parts have blocks / parts steps, and every CTA of a cluster needs one)
+        for (int split = 1; split <= 8 && split <= blocks / parts; split *= 2) {
             const int64_t at_once = clusters_at_once(split, sms), rounds = (small * parts + at_once - 1) / at_once;
             const double c = join + 1.0 + (double)rounds * (4.6 + 0.45 * ((b + split - 1) / split) + (split > 1 ? 1.5 : 0.0));
             if (c < cost - 0.05) { cost = c; best = {false, false, split, parts, small}; }

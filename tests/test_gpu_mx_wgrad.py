@@ -56,6 +56,19 @@ def test_sizes(M, N, K, accumulate):
     check(dy, v, dw, M, base if accumulate else None)
 
 
+@pytest.mark.parametrize("N,K", [(24, 40), (130, 250), (520, 300)])
+def test_every_number_of_steps(N, K):
+    """However the 64-token steps divide among parts and the CTAs of a cluster: the first tokens of one input, 1 to 130 steps, the last
+    step short."""
+    dy, c, s, v = inputs(N + K, 130 * 64, N, K)
+    for steps in range(1, 131):
+        M = steps * 64 - steps % 3
+        dw = torch.full((N, K), float("nan"), device="cuda")
+        sparq.sparq_wgrad_mx8(dy[:M], c[:M], s[:M], dw)
+        sparq.sparq_check()
+        check(dy[:M], v[:M], dw, M, None)
+
+
 @pytest.mark.parametrize("M,N,K", [(65536, 256, 256), (100000, 2048, 512)])
 def test_long_sums_keep_32_bits(M, N, K):
     """All terms of one sign, where a sum that is cut off instead of rounded drifts: the relative error stays below 2^-19, twice what 48 cut
