@@ -7,7 +7,9 @@
 // s the logistic function: act' = s + x s (1 - s) z'.
 //
 // A thread takes 16 elements of a row as in sparq_mx.cu.  Every tensor is read and written once: HBM traffic is the bound,
-// 7 bytes forward and 8 backward per element of a gated bf16 pair.
+// 8 bytes and a sixteenth forward and backward per element of a gated bf16 pair.  8192 x 8192, gated silu: forward 94.8 us (5.7 TB/s),
+// backward 99.4 (5.5), where a copy reaches 6.55; at 64 registers half of an SM's warps fit, and the arithmetic (a power of two and
+// a reciprocal an element, 2.8 instructions a cycle) takes most of the issue slots that the loads leave.
 #include "sparq_mx.cuh"
 
 namespace sparq {

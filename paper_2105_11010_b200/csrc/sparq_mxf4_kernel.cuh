@@ -11,6 +11,9 @@
 // Tensor memory: 464 columns of accumulators, 48 of scales.  Two accumulators of 256 columns do not fit, so they share 48
 // columns: the epilogue empties those first (columns 208..255), and the next tile's first MMA waits for no more than that.
 //
+// 16384 x 4096 x 4096 NVFP4 94.8 us, 5.8 PFLOP/s: 0.90 of four times cuBLAS's bf16 rate in a burst, and at the power cap.  8192 rows:
+// 638 MB of operands from L2 for 29 MB from HBM.
+//
 // Warps: 0 producer of the codes, 10 of the scales, 1 tensor memory and (leader) MMA issue, 2..9 epilogue (lane quarter warp % 4, two spans of 64 columns).
 #pragma once
 

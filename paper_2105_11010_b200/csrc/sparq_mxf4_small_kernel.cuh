@@ -5,7 +5,8 @@
 //
 // A tile is 128 rows of one operand (the MMA's M side, accumulator lanes) x BN rows of the other (columns).
 //   SWAP     lanes are rows of B (a layer's weights), columns 16 or 32 rows of A: one token costs one pass over the weights and
-//            16 columns of tensor memory, and a warp's store of one token's outputs is contiguous.
+//            16 columns of tensor memory, and a warp's store of one token's outputs is contiguous.  1 x 8192 x 8192 NVFP4 7.8 us,
+//            4.8 TB/s of weights; 1 x 16384 x 8192 11.9, 6.3 TB/s.
 //   else     lanes are rows of A, columns 128 rows of B: a lane holds runs of an output row, stored 32 bytes at a time.
 //            (64 tokens as columns: 64 x 2048, K 512, 4.8 us, 128 tokens 7.2, most of it two-byte stores.)
 //

@@ -22,7 +22,7 @@ cudaError_t launch_wgrad(Kernel kernel, bool (&attr_set)[64], int grid, int clus
 struct WgradForm {
     bool pairs, expand;     // pairs of CTAs on 256 x 256 tiles, X expanded to bf16 first
     int split, parts;
-    int64_t tiles;
+    int64_t tiles, whole;   // whole: tiles in front that are not cut into the parts
 };
 
 // By estimates of the time in us, fitted to launches of 64 to 100352 tokens and 64 x 256 to 2048 x 2048 outputs in every form: the choice is
@@ -33,6 +33,7 @@ WgradForm pick_wgrad(int64_t M, int64_t N, int64_t K, int blocks, int sms)
 {
     WgradForm best = {};
     double cost = 1e30;
+    const bool x16_fits = (double)M * (double)mx_padded(K) * 2.0 <= (double)kWorkspaceMaxBytes;
     const int64_t small = (N + 127) / 128 * ((K + 127) / 128), large = (N + 255) / 256 * ((K + 255) / 256);
     const double expand = 1.5 + (double)M * (double)K * 3.0 / 6.0e6;
     for (int parts = 1; parts <= 128 && parts * 8 <= blocks + 7; parts += parts < 8 ? 1 : parts < 32 ? 4 : 16) {
@@ -43,12 +44,21 @@ WgradForm pick_wgrad(int64_t M, int64_t N, int64_t K, int blocks, int sms)
         for (int split = 1; split <= 8 && split <= blocks / parts; split *= 2) {
             const int64_t at_once = clusters_at_once(split, sms), rounds = (small * parts + at_once - 1) / at_once;
             const double c = join + 1.0 + (double)rounds * (4.6 + 0.45 * ((b + split - 1) / split) + (split > 1 ? 1.5 : 0.0));
-            if (c < cost - 0.05) { cost = c; best = {false, false, split, parts, small}; }
+            if (c < cost - 0.05) { cost = c; best = {false, false, split, parts, small, 0}; }
         }
         const int64_t rounds = (large * parts + sms / 2 - 1) / (sms / 2);
         const double q = join + 7.0 + (double)rounds * 0.48 * b, x = join + 7.0 + expand + (double)rounds * 0.36 * b;
-        if (q < cost - 0.05) { cost = q; best = {true, false, 1, parts, large}; }
-        if (x < cost - 0.05 && (double)M * (double)mx_padded(K) * 2.0 <= (double)kWorkspaceMaxBytes) { cost = x; best = {true, true, 1, parts, large}; }
+        if (q < cost - 0.05) { cost = q; best = {true, false, 1, parts, large, 0}; }
+        if (x < cost - 0.05 && x16_fits) { cost = x; best = {true, true, 1, parts, large, 0}; }
+    }
+    // Whole tiles but for a last round that leaves most pairs without one, whose tiles are cut (256 tiles on 74 pairs: 3 rounds and
+    // a half for 4; 16384 x 4096 x 4096 433 us, in two parts throughout 490; 4100 x 2560 x 2040 55 and 67).
+    const int64_t pairs = sms / 2, tail = large % pairs;
+    for (int parts = 2; parts <= 8 && parts * 8 <= blocks && large > pairs && tail > 0; ++parts) {
+        const double b = (double)(large / pairs) * blocks + (double)((tail * parts + pairs - 1) / pairs) * ((blocks + parts - 1) / parts);
+        const double join = 3.0 + (double)(2 * parts * tail) * (kWgTile * kWgTile * 4.0 / 5.0e6), q = join + 7.0 + 0.48 * b, x = join + 7.0 + expand + 0.36 * b;
+        if (q < cost - 0.05) { cost = q; best = {true, false, 1, parts, large, large - tail}; }
+        if (x < cost - 0.05 && x16_fits) { cost = x; best = {true, true, 1, parts, large, large - tail}; }
     }
     return best;
 }
@@ -59,7 +69,10 @@ struct Scratch {
 Scratch scratch_of(const WgradForm &f, int64_t M, int64_t N, int64_t K)
 {
     auto round = [](size_t b) { return (b + 255) / 256 * 256; };
-    return {f.expand ? round((size_t)M * (size_t)mx_padded(K) * 2) : 0, f.parts > 1 ? round((size_t)f.parts * (size_t)N * (size_t)K * sizeof(float)) : 0};
+    return {f.expand ? round((size_t)M * (size_t)mx_padded(K) * 2) : 0, 
+            f.parts == 1 ? 0
+            : f.whole ? (size_t)(f.parts - 1) * (size_t)(f.tiles - f.whole) * kWgTile * kWgTile * sizeof(float)
+                      : round((size_t)f.parts * (size_t)N * (size_t)K * sizeof(float))};
 }
 
 }  // namespace
@@ -139,19 +152,22 @@ extern "C" int sparq_wgrad_mx8(const void *dy, int64_t lddy, const int8_t *codes
         if (rc == SPARQ_OK) rc = encode_matrix(&map_x, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, x, K, M, pitch * 2, 64, kWgTokens, CU_TENSOR_MAP_SWIZZLE_128B);
     }
     const int launches = sums ? 1 : g.parts;
-    if (sums) {
+    if (sums && form.whole == 0) {
         g.dw = sums;
         g.part_stride = N * K;
         g.accumulate = 0;
     }
     g.count = sums ? g.parts : 1;
+    WgradPairArgs p = {g, (int)((N + kWgTile - 1) / kWgTile), (int)((K + kWgTile - 1) / kWgTile), 0, (int)form.whole, 0, form.whole ? sums : nullptr};
     for (int l = 0; l < launches && rc == SPARQ_OK; ++l) {
         g.part = l;
         if (!sums) g.accumulate = accumulate != 0 || l > 0;
         cudaError_t e;
         if (form.pairs) {
-            const int64_t items = form.tiles * g.count;
-            const WgradPairArgs p = {g, (int)((N + kWgTile - 1) / kWgTile), (int)((K + kWgTile - 1) / kWgTile), (int)(items < sms / 2 ? items : sms / 2)};
+            p.g = g;
+            p.skip = form.whole && l > 0;
+            const int64_t items = (p.skip ? 0 : form.whole) + (form.tiles - form.whole) * g.count;
+            p.pairs = (int)(items < sms / 2 ? items : sms / 2);
             static bool set_x[64] = {}, set_q[64] = {};
             e = x ? launch_wgrad(sparq_wgrad_kernel<true>, set_x, 2 * p.pairs, 2, kWgPairThreads, wgrad_smem(true), st, map_dy, map_x, map_x, p)
                   : launch_wgrad(sparq_wgrad_kernel<false>, set_q, 2 * p.pairs, 2, kWgPairThreads, wgrad_smem(false), st, map_dy, map_codes, map_scales, p);
@@ -162,7 +178,10 @@ extern "C" int sparq_wgrad_mx8(const void *dy, int64_t lddy, const int8_t *codes
         }
         if (e != cudaSuccess) rc = cuda_error(e, "weight gradient kernel launch");
     }
-    if (sums && rc == SPARQ_OK) {
+    if (sums && form.whole && rc == SPARQ_OK) {
+        const cudaError_t e = launch_overlapped(wgrad_add_tail_kernel, (int)(form.tiles - form.whole) * (kWgTile / kWgAddRows), kWgTile, 0, st, p);
+        if (e != cudaSuccess) rc = cuda_error(e, "wgrad_add_tail_kernel launch");
+    } else if (sums && rc == SPARQ_OK) {
         const int64_t threads = (N * K + 3) / 4, blocks = (threads + 255) / 256;
         const cudaError_t e = launch_overlapped(wgrad_add_parts_kernel, (int)(blocks < 8 * sms ? blocks : 8 * sms), 256, 0, st, (const float *)sums, N * K,
                                                 g.parts, (int)(accumulate != 0), dw);

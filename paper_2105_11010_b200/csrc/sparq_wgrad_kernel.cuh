@@ -279,7 +279,7 @@ struct WgradSmall : WgradCta<6, 4> {
     __device__ void work(const WgradArgs &g, float (&sum)[kWgOwn]) const
     {
         // A team of four warps takes every fourth stage: a stage's chain of barriers, loads, arithmetic and stores is mostly latency, which the
-        // other teams' fill (two teams: 0.51 us a step, of which 0.3 are there without any transform).
+        // other teams' fill (100352 x 128 x 1152: four teams 54.8 us, two 59.5, of which 36 are there without any transform).
         const int team = (warp - 2) >> 2;
         const TeamPlace place((threadIdx.x - 64) & 127, (int)(k0 / 32) & 15, kWgCodes, kWgScales, 0);
 #pragma unroll
@@ -452,10 +452,11 @@ sparq_wgrad_small_kernel(const __grid_constant__ CUtensorMap map_dy, const __gri
 // ---- many output tiles -----------------------------------------------------------------------------------
 // A persistent pair of CTAs walks tiles of 256 x 256: one MMA (cta_group::2) multiplies 256 columns of dy by 256 of X.  Each CTA
 // brings its 128 columns of dy, and brings and transforms its 128 columns of X: a value of X is transformed once per row of tiles
-// of 256, half as often as with one CTA by itself, and neither the transform (8192 values a step and SM, about 200 of
-// its 512 cycles of issue) nor shared memory (81 KB a step, of 64 KB the MMAs alone) holds the tensor cores up much.
-// X16: X comes as bf16 (the library's own, expanded from the codes by the launch before) and goes from TMA to the MMA; the workers
-// only add up.  Same operands, same order of sums, same bits.
+// of 256, half as often as with one CTA by itself.  A step of 64 tokens takes 0.48 us: the chain from the codes' arrival
+// through the transform to the MMA, more than any pipe.
+// X16: X comes as bf16 (the library's own, expanded from the codes by the launch before) and goes from TMA to the MMA, 0.36 us a step;
+// the workers only add up.  Same operands, same order of sums, same bits.  16384 x 4096 x 4096 513 us with the expansion's 35, 1.07
+// PFLOP/s in all, at the power cap; 8192 tokens: tensor pipe 72 % active, with 256 tiles in four rounds on 74 pairs (3.46 would do).
 // Warps: 0 producer of dy, 2 of codes and scales, 1 tensor memory and (leader) MMA issue, 4..11 workers, each thread with 128
 // columns of a row in registers.
 
@@ -469,26 +470,41 @@ constexpr int kWgPairThreads = 32 * (kWgFirstWorker + kWgPairWorkers);
 constexpr int kWgStages16 = 7;
 __host__ __device__ constexpr int wgrad_smem(bool x16) { return 1024 + (x16 ? kWgStages16 * 4 * kWgBox : WgradCta<7, 3>::kRings); }
 
+// The first `whole` tiles run over all tokens, the others (the tail) over the parts that the launch takes.  Where those follow whole tiles,
+// the first part's sums go to dw, the others' into tail_sums, 256 x 256 for each tile, or in launches of their own (skip: of the tail only)
+// to dw too.
 struct WgradPairArgs {
     WgradArgs g;
-    int n_tiles, k_tiles, pairs;
+    int n_tiles, k_tiles, pairs, whole, skip;
+    float *tail_sums;
 };
 
 // Steps of part p.
 __device__ __forceinline__ int part_begin(const WgradArgs &g, int p) { return (int)((int64_t)p * g.blocks / g.parts); }
 
-// Item t: its part, and its tile in an order that keeps eight rows of tiles together.
-__device__ __forceinline__ void wgrad_tile(const WgradPairArgs &p, int t, int &part, int &nt, int &kt)
+// Tile t in an order that keeps eight rows of tiles together.
+__device__ __forceinline__ void wgrad_tile(int n_tiles, int k_tiles, int t, int &nt, int &kt)
 {
-    const int tiles = p.n_tiles * p.k_tiles;
-    part = t / tiles;
-    t -= part * tiles;
-    part += p.g.part;
-    const int per_group = 8 * p.k_tiles, group = t / per_group, first = group * 8;
-    const int rows = p.n_tiles - first < 8 ? p.n_tiles - first : 8, in = t - group * per_group;
+    const int per_group = 8 * k_tiles, group = t / per_group, first = group * 8;
+    const int rows = n_tiles - first < 8 ? n_tiles - first : 8, in = t - group * per_group;
     kt = in / rows;
     nt = first + in - kt * rows;
 }
+
+// Item t of a launch: its tile, its steps, and which part of the tail's tile `at` it is (whole tiles: part 0).
+struct WgradItem {
+    int nt, kt, part, at, first, last;
+    __device__ WgradItem(const WgradPairArgs &p, int t)
+    {
+        const int tail = p.n_tiles * p.k_tiles - p.whole, u = p.skip ? t : t - p.whole;
+        part = u < 0 ? 0 : u / tail;
+        at = u - part * tail;
+        wgrad_tile(p.n_tiles, p.k_tiles, p.whole + at, nt, kt);
+        part += u < 0 ? 0 : p.g.part;
+        first = u < 0 ? 0 : part_begin(p.g, part);
+        last = u < 0 ? p.g.blocks : part_begin(p.g, part + 1);
+    }
+};
 
 // full: dy of both CTAs, in the leader; raw: codes and scales of this CTA; xf: transformed by both CTAs' workers,
 // in the leader; empty: the MMAs that read the stage have retired; acc, freed: as above.
@@ -508,10 +524,9 @@ struct WgradPair : WgradCta<7, 3> {
             uint32_t ph = 1;
             bool live = true;
             for (int t = pair; t < tiles && live; t += p.pairs) {
-                int part, nt, kt;
-                wgrad_tile(p, t, part, nt, kt);
-                const int n = nt * kWgTile + rank * 128, k = kt * kWgTile + rank * 128, sc = (k / 32) & ~15;
-                for (int b = part_begin(g, part), last = part_begin(g, part + 1); b < last; ++b) {
+                const WgradItem item(p, t);
+                const int n = item.nt * kWgTile + rank * 128, k = item.kt * kWgTile + rank * 128, sc = (k / 32) & ~15;
+                for (int b = item.first; b < item.last; ++b) {
                     if (used >= kStages && !mbar_wait(empty_bar(s), ph, abort_flag, g.status, g.wait_limit)) { live = false; break; }
                     const uint32_t at = smem + (uint32_t)(s * kStage);
                     const int m = b * kWgTokens;
@@ -558,7 +573,8 @@ struct WgradPair : WgradCta<7, 3> {
             RingAt<kX> x;
             int c = 0;
             for (int t = pair; t < tiles; t += p.pairs) {
-                const int part = g.part + t / (p.n_tiles * p.k_tiles), steps_of = part_begin(g, part + 1) - part_begin(g, part);
+                const WgradItem item(p, t);
+                const int steps_of = item.last - item.first;
                 for (int b = 0; b < steps_of; ++b) {
                     const int in = b & (kWgChunkSteps - 1);
                     if (in == 0 && c >= 2) mbar_wait_warp(elected, freed_bar(c & 1), (uint32_t)((c >> 1) - 1) & 1u, abort_flag, g.status, g.wait_limit);
@@ -603,9 +619,16 @@ struct WgradPair : WgradCta<7, 3> {
         if (lane == 0) mbar_arrive_remote(leader_freed + 8u * (uint32_t)(c & 1));
     }
 
-    __device__ void write(const WgradArgs &g, float *dw, int64_t n, int64_t k, const float (&sum)[kWgPairOwn]) const
+    __device__ void write(const WgradPairArgs &p, const WgradItem &item, const float (&sum)[kWgPairOwn]) const
     {
-        if (n < g.N && k < g.K) wgrad_put_row(dw + n * g.K + k, sum, g.K - k, g.accumulate, [](int j) { return X16 ? j : wgrad_column(j); });
+        const WgradArgs &g = p.g;
+        const int row = rank * 128 + (warp & 3) * 32 + lane, col = ((warp - kWgFirstWorker) >> 2) * kWgPairOwn;
+        const int64_t n = (int64_t)item.nt * kWgTile + row, k = (int64_t)item.kt * kWgTile + col;
+        if (n >= g.N || k >= g.K) return;
+        const bool aside = p.tail_sums && item.part > 0;
+        float *to = aside ? p.tail_sums + (((int64_t)(item.part - 1) * (p.n_tiles * p.k_tiles - p.whole) + item.at) * kWgTile + row) * kWgTile + col
+                          : g.dw + (item.part - g.part) * g.part_stride + n * g.K + k;
+        wgrad_put_row(to, sum, g.K - k, aside ? 0 : g.accumulate, [](int j) { return X16 ? j : wgrad_column(j); });
     }
 
     __device__ void work(const WgradPairArgs &p) const
@@ -618,10 +641,9 @@ struct WgradPair : WgradCta<7, 3> {
         RingAt<kX> x;
         int c = 0, stage = 0;
         for (int t = pair; t < tiles; t += p.pairs) {
-            int part, nt, kt;
-            wgrad_tile(p, t, part, nt, kt);
-            const int steps_of = part_begin(g, part + 1) - part_begin(g, part);
-            const TeamPlace place(threadIdx.x & 127, ((kt * kWgTile + rank * 128) / 32) & 15, kWgCodes, kWgScales, 0);
+            const WgradItem item(p, t);
+            const int steps_of = item.last - item.first;
+            const TeamPlace place(threadIdx.x & 127, ((item.kt * kWgTile + rank * 128) / 32) & 15, kWgCodes, kWgScales, 0);
             float sum[kWgPairOwn];
 #pragma unroll
             for (int j = 0; j < kWgPairOwn; ++j) sum[j] = 0.0f;
@@ -648,7 +670,7 @@ struct WgradPair : WgradCta<7, 3> {
             if (c > c_first) add_chunk(g, c - 1, leader_freed, sum);
             add_chunk(g, c, leader_freed, sum);
             ++c;
-            write(g, g.dw + (part - g.part) * g.part_stride, (int64_t)nt * kWgTile + rank * 128 + (warp & 3) * 32 + lane, (int64_t)kt * kWgTile + ((warp - kWgFirstWorker) >> 2) * kWgPairOwn, sum);
+            write(p, item, sum);
         }
     }
 };
@@ -671,7 +693,7 @@ sparq_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_cons
     c.bars = smem_u32(&room);
     c.rank = (int)(blockIdx.x & 1u);
     c.pair = (int)(blockIdx.x >> 1);
-    c.tiles = p.n_tiles * p.k_tiles * p.g.count;
+    c.tiles = (p.skip ? 0 : p.whole) + (p.n_tiles * p.k_tiles - p.whole) * p.g.count;
 
     if (warp == 0) {
         if (lane == 0) {
@@ -728,6 +750,32 @@ sparq_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_cons
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" :: "r"(c.tmem), "r"(512u) : "memory");
     }
+}
+
+// dw += the sums of the tail's later parts, one after the other; a block takes kWgAddRows rows of a tile.
+constexpr int kWgAddRows = 4;
+__global__ void __launch_bounds__(kWgTile)
+wgrad_add_tail_kernel(const WgradPairArgs p)
+{
+    const int per_tile = kWgTile / kWgAddRows, at = (int)blockIdx.x / per_tile, row = ((int)blockIdx.x - at * per_tile) * kWgAddRows;
+    int nt, kt;
+    wgrad_tile(p.n_tiles, p.k_tiles, p.whole + at, nt, kt);
+    const int64_t n = (int64_t)nt * kWgTile + row, k = (int64_t)kt * kWgTile + threadIdx.x, part = (int64_t)(p.n_tiles * p.k_tiles - p.whole) * kWgTile * kWgTile;
+    const float *from = p.tail_sums + ((int64_t)at * kWgTile + row) * kWgTile + threadIdx.x;
+    float *dw = p.g.dw + n * p.g.K + k;
+    dep_wait();
+    dep_launch();
+    if (k >= p.g.K) return;
+    float a[kWgAddRows];
+#pragma unroll
+    for (int r = 0; r < kWgAddRows; ++r) a[r] = n + r < p.g.N ? dw[r * p.g.K] : 0.0f;
+#pragma unroll 4
+    for (int q = 1; q < p.g.parts; ++q, from += part)
+#pragma unroll
+        for (int r = 0; r < kWgAddRows; ++r) a[r] = __fadd_rn(a[r], n + r < p.g.N ? from[r * kWgTile] : 0.0f);
+#pragma unroll
+    for (int r = 0; r < kWgAddRows; ++r)
+        if (n + r < p.g.N) dw[r * p.g.K] = a[r];
 }
 
 // dw (+)= the parts' sums, one after the other.

@@ -1,7 +1,7 @@
 """Activation functions that keep their inputs in 8 bits, and their backward pass, against the formulas in 64 bits.
 
-Tolerance.  The kernels work in fp32 with CUDA's __expf (2 + |1.16 z| units of 2^-23) and __fdividef (2 units).  With E that error of
-exp(-z) and z itself off by 4 roundings (4 |z| 2^-24), s(z) = 1 / (1 + exp(-z)) is off by s (1 - s) (E + 2 |z| 2^-23) + 3 s 2^-23,
+Tolerance.  The kernels work in fp32 with the approximate power of two (exp(-z) off by 2 + |1.16 z| units of 2^-23, the multiplication by log2 e
+included) and reciprocal (1 unit).  With E that error of exp(-z) and z itself off by 4 roundings (4 |z| 2^-24), s(z) = 1 / (1 + exp(-z)) is off by s (1 - s) (E + 2 |z| 2^-23) + 3 s 2^-23,
 written as s e; products add 2^-24 each.  The derivative s + c s (1 - s) z' is off by s e, |c z'| times the errors of s (1 - s), and
 five roundings of the second term.  bf16 outputs add half a step, 2^-8 of the result."""
 import numpy as np

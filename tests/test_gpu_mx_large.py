@@ -96,8 +96,9 @@ def kept(x):
     return c, s, v.double()
 
 
-# one part and several, both tile sizes, expanded first and not
-WGRADS = [(200, 2304, 2304), (6000, 2600, 2600), (5000, 1000, 1100), (30000, 300, 700), (9001, 72, 300), (40000, 128, 1152), (3000, 4100 // 8 * 8, 513)]
+# one part and several, both tile sizes, expanded first and not, tiles of a last round in parts (the last four)
+WGRADS = [(200, 2304, 2304), (6000, 2600, 2600), (5000, 1000, 1100), (30000, 300, 700), (9001, 72, 300), (40000, 128, 1152), (3000, 4100 // 8 * 8, 513),
+          (4100, 2560, 2040), (2500, 2504, 2003), (1500, 2490, 2001), (4096, 4096, 4096)]
 
 
 @pytest.mark.parametrize("M,N,K", WGRADS)
