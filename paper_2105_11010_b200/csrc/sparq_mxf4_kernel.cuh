@@ -11,8 +11,9 @@
 // Tensor memory: 464 columns of accumulators, 48 of scales.  Two accumulators of 256 columns do not fit, so they share 48
 // columns: the epilogue empties those first (columns 208..255), and the next tile's first MMA waits for no more than that.
 //
-// 16384 x 4096 x 4096 NVFP4 94.8 us, 5.8 PFLOP/s: 0.90 of four times cuBLAS's bf16 rate in a burst, and at the power cap.  8192 rows:
-// 638 MB of operands from L2 for 29 MB from HBM.
+// 16384 x 4096 x 4096 NVFP4 to bf16 109 us call after call, 127 with L2 emptied in between; 8192 x 8192 x 8192 201 us, 5.5 PFLOP/s, 0.84
+// of four times cuBLAS's bf16 rate in a burst.  What bounds it is the way from L2 to the SMs: 8192 x 4096 x 4096 takes in 638 MB of
+// operands (29 MB of them from HBM) in 57 us, 11 TB/s or 7 KB a cycle, with the tensor pipe 62 % active; and the power cap.
 //
 // Warps: 0 producer of the codes, 10 of the scales, 1 tensor memory and (leader) MMA issue, 2..9 epilogue (lane quarter warp % 4, two spans of 64 columns).
 #pragma once

@@ -279,7 +279,7 @@ struct WgradSmall : WgradCta<6, 4> {
     __device__ void work(const WgradArgs &g, float (&sum)[kWgOwn]) const
     {
         // A team of four warps takes every fourth stage: a stage's chain of barriers, loads, arithmetic and stores is mostly latency, which the
-        // other teams' fill (100352 x 128 x 1152: four teams 54.8 us, two 59.5, of which 36 are there without any transform).
+        // other teams' fill (100352 x 128 x 1152 call after call: four teams 54.8 us, two 59.5, of which 36 are there without any transform).
         const int team = (warp - 2) >> 2;
         const TeamPlace place((threadIdx.x - 64) & 127, (int)(k0 / 32) & 15, kWgCodes, kWgScales, 0);
 #pragma unroll
@@ -455,8 +455,9 @@ sparq_wgrad_small_kernel(const __grid_constant__ CUtensorMap map_dy, const __gri
 // of 256, half as often as with one CTA by itself.  A step of 64 tokens takes 0.48 us: the chain from the codes' arrival
 // through the transform to the MMA, more than any pipe.
 // X16: X comes as bf16 (the library's own, expanded from the codes by the launch before) and goes from TMA to the MMA, 0.36 us a step;
-// the workers only add up.  Same operands, same order of sums, same bits.  16384 x 4096 x 4096 513 us with the expansion's 35, 1.07
-// PFLOP/s in all, at the power cap; 8192 tokens: tensor pipe 72 % active, with 256 tiles in four rounds on 74 pairs (3.46 would do).
+// the workers only add up.  Same operands, same order of sums, same bits.  16384 x 4096 x 4096 433 us call after call with
+// the expansion's 35 (469 with L2 emptied in between), 1.27 PFLOP/s in all, at the power cap; 8192 tokens, in whole tiles: 11 TB/s of operands
+// from L2, tensor pipe 72 % active (four rounds for 3.46).
 // Warps: 0 producer of dy, 2 of codes and scales, 1 tensor memory and (leader) MMA issue, 4..11 workers, each thread with 128
 // columns of a row in registers.
 
