@@ -378,8 +378,8 @@ SPARQ_API int sparq_act_forward_mx8(const void *x, const void *up, int dtype, in
 
 /* The backward pass, from the kept values x^ and up^:
  *     dx = dy * act'(x^);  with up: dx = (dy * up^) * act'(x^), dup = dy * act(x^).
- * dx and dup share lddx; dx or dup may be dy itself (same leading dimension).  A block that reads as NaN gives
- * NaN. */
+ * dx and dup share lddx and are two matrices; dx or dup may be dy itself (same leading dimension).  A block that
+ * reads as NaN gives NaN. */
 SPARQ_API int sparq_act_backward_mx8(const void *dy, int dtype, int64_t rows, int64_t cols, int64_t lddy, int act,
                            const int8_t *codes, const uint8_t *scales, const int8_t *up_codes, const uint8_t *up_scales,
                            void *dx, void *dup, int64_t lddx, void *stream);

@@ -221,6 +221,7 @@ extern "C" int sparq_act_forward_mx8(const void *x, const void *up, int dtype, i
     rc = check_pitches(dtype, rows, cols, ldx, ldy, (uintptr_t)x | (uintptr_t)up | (uintptr_t)y,
                        (uintptr_t)codes | (uintptr_t)scales | (uintptr_t)up_codes | (uintptr_t)up_scales);
     if (rc != SPARQ_OK) return rc;
+    if ((y == x || y == up) && ldy != ldx && rows > 1) return set_error(SPARQ_ERR_INVALID_ARG, "y in place of x or up has their leading dimension");
     const bool bf16 = dtype == SPARQ_DTYPE_BF16;
     const int width = bf16 ? 2 : 4;
     const int align = min_align(min_align(run_align(x, ldx, width), run_align(y, ldy, width)), up ? run_align(up, ldx, width) : 32);
@@ -243,6 +244,8 @@ extern "C" int sparq_act_backward_mx8(const void *dy, int dtype, int64_t rows, i
     rc = check_pitches(dtype, rows, cols, lddy, lddx, (uintptr_t)dy | (uintptr_t)dx | (uintptr_t)dup,
                        (uintptr_t)codes | (uintptr_t)scales | (uintptr_t)up_codes | (uintptr_t)up_scales);
     if (rc != SPARQ_OK) return rc;
+    if ((dx == dy || dup == dy) && lddx != lddy && rows > 1) return set_error(SPARQ_ERR_INVALID_ARG, "dx or dup in place of dy has its leading dimension");
+    if (dx == dup) return set_error(SPARQ_ERR_INVALID_ARG, "dx and dup are one matrix");
     const bool bf16 = dtype == SPARQ_DTYPE_BF16;
     const int width = bf16 ? 2 : 4;
     const int align = min_align(min_align(run_align(dy, lddy, width), run_align(dx, lddx, width)), dup ? run_align(dup, lddx, width) : 32);

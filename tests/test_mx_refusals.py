@@ -107,6 +107,13 @@ def test_act(forward):
     refused(-2, "aligned", call(codes=P + 8))
     refused(-2, "aligned", call(up=P, uc=P, us=P + 1))
     refused(-2, "2^31", call(rows=1 << 41))
+    refused(-1, "in place", call(ldy=72))
+    refused(-1, "in place", call(ld=72))
+    if forward:
+        refused(-1, "in place", call(up=P + 4096, uc=P, us=P, y=P + 4096, ld=72))
+    else:
+        refused(-1, "in place", call(up=P, uc=P, us=P, y=P + 4096, ld=72))
+        refused(-1, "one matrix", call(x=P + 8192, up=P, uc=P, us=P))
     assert call(rows=0, x=None) == 0 and call(cols=0, x=None) == 0
 
 
