@@ -289,8 +289,12 @@ struct WgradSmall : WgradCta<6, 4> {
         int c = 0;
         for (int it = 0; it < steps; ++it) {
             if (it % kWgTeams == team) {
-                mbar_wait_warp(lane == 0 ? 1u : 0u, raw_bar(raw.s), raw.ph, abort_flag, g.status, g.wait_limit);
+                // The X stage first: its MMA, of step it - kX, comes behind that of step it - kRaw, whose phase of the raw barrier, another
+                // team's to wait for, is complete then.  A barrier tells a phase from the next only, so that before it a wait for this step's
+                // would return at once.
+                static_assert(kX <= kRaw, "the X stage's last step is not older than the raw stage's");
                 if (it >= kX) mbar_wait_warp(lane == 0 ? 1u : 0u, x_empty_bar(x.s), x.ph ^ 1u, abort_flag, g.status, g.wait_limit);
+                mbar_wait_warp(lane == 0 ? 1u : 0u, raw_bar(raw.s), raw.ph, abort_flag, g.status, g.wait_limit);
                 transform_stage(smem + (uint32_t)(raw.s * kWgStage), x_stage(x.s), place);
                 fence_proxy_async_smem();
                 __syncwarp();
@@ -652,8 +656,9 @@ struct WgradPair : WgradCta<7, 3> {
             for (int b = 0; b < steps_of; ++b) {
                 if (!X16) {
                     if ((stage & 1) == team) {
-                        mbar_wait_warp(lane == 0 ? 1u : 0u, raw_bar(raw.s), raw.ph, abort_flag, g.status, g.wait_limit);
+                        // the X stage first, as above
                         if (stage >= kX) mbar_wait_warp(lane == 0 ? 1u : 0u, x_empty_bar(x.s), x.ph ^ 1u, abort_flag, g.status, g.wait_limit);
+                        mbar_wait_warp(lane == 0 ? 1u : 0u, raw_bar(raw.s), raw.ph, abort_flag, g.status, g.wait_limit);
                         transform_stage(smem + (uint32_t)(raw.s * kStage), x_stage(x.s), place);
                         fence_proxy_async_smem();
                         __syncwarp();

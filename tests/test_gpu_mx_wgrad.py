@@ -153,6 +153,24 @@ def test_same_bits_every_time(M, N, K):
     assert all(torch.equal(g, got[0]) for g in got)
 
 
+@pytest.mark.parametrize("M,N,K", [(17356, 2607, 1), (18400, 2675, 3), (20270, 2044, 94), (3499, 4717, 147), (4100, 2560, 2040)])
+def test_same_bits_with_cold_caches(M, N, K):
+    """Loads that come late and out of order: 300 calls with L2 emptied in between (half of them) give the first call's bits."""
+    dy, c, s, v = inputs(9, M, N, K)
+    first = torch.empty((N, K), device="cuda")
+    sparq.sparq_wgrad_mx8(dy, c, s, first)
+    check(dy, v, first, M)
+    flush = torch.empty(160 << 18, device="cuda")
+    dw, differ = torch.empty((N, K), device="cuda"), torch.zeros((), dtype=torch.int64, device="cuda")
+    for i in range(300):
+        if i & 1:
+            flush.fill_(i)
+        sparq.sparq_wgrad_mx8(dy, c, s, dw)
+        differ += (dw != first).any()
+    sparq.sparq_check()
+    assert int(differ) == 0
+
+
 def test_gradient_against_differences():
     """The loss sum(dy * (X w^T)) is linear in w: its difference quotient over any step is the gradient, up to the rounding of 64 bits."""
     M, N, K = 200, 16, 40
