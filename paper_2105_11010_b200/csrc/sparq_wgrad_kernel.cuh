@@ -460,7 +460,7 @@ sparq_wgrad_small_kernel(const __grid_constant__ CUtensorMap map_dy, const __gri
 // through the transform to the MMA, more than any pipe.
 // X16: X comes as bf16 (the library's own, expanded from the codes by the launch before) and goes from TMA to the MMA, 0.36 us a step;
 // the workers only add up.  Same operands, same order of sums, same bits.  16384 x 4096 x 4096 433 us call after call with
-// the expansion's 35 (469 with L2 emptied in between), 1.27 PFLOP/s in all, at the power cap; 8192 tokens, in whole tiles: 11 TB/s of operands
+// the expansion's 35 (457 with L2 emptied in between), 1.27 PFLOP/s in all, at the power cap; 8192 tokens, in whole tiles: 11 TB/s of operands
 // from L2, tensor pipe 72 % active (four rounds for 3.46).
 // Warps: 0 producer of dy, 2 of codes and scales, 1 tensor memory and (leader) MMA issue, 4..11 workers, each thread with 128
 // columns of a row in registers.
