@@ -90,7 +90,8 @@ __host__ __device__ constexpr int tmem_columns(int want) { return want <= 32 ? 3
 
 // mbar_wait of a converged warp through one of its lanes.  Every lane's own look at a barrier, complete or not, takes its turn: about
 // 130 cycles for 32 of them, which in a loop of a few hundred cycles is what the loop takes.  The lanes decide together, by votes, so
-// that the warp stays converged for the instructions behind the wait that need it to be.
+// that the warp stays converged for the instructions behind the wait that need it to be; __syncwarp makes what the one lane has
+// seen come before what the others do.
 __device__ __forceinline__ bool mbar_try_wait_of(uint32_t mine, uint32_t bar, uint32_t parity)
 {
     uint32_t ok;
@@ -101,7 +102,9 @@ __device__ __forceinline__ bool mbar_try_wait_of(uint32_t mine, uint32_t bar, ui
         "@q mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
         "selp.u32 %0, 1, 0, p;\n\t}"
         : "=r"(ok) : "r"(bar), "r"(parity), "r"(mine) : "memory");
-    return __any_sync(0xFFFFFFFFu, ok);
+    const bool any = __any_sync(0xFFFFFFFFu, ok);
+    __syncwarp();
+    return any;
 }
 __device__ __forceinline__ void mbar_wait_warp(uint32_t mine, uint32_t bar, uint32_t parity, volatile uint32_t *abort_flag, unsigned int *status,
                                                long long limit_cycles)
