@@ -178,6 +178,8 @@ template <int R, int X>
 struct WgradCta : MxCta {
     static constexpr int kRaw = R, kX = X, kRings = R * kWgStage + X * kWgXStage;
     static_assert(R <= kMaxStages && X <= kMaxStages, "a barrier for each stage");
+    // A wait for a step's raw stage comes behind the wait for its X stage, whose MMA is behind that of the raw stage's last use.
+    static_assert(X <= R, "the X stage's last step is not older than the raw stage's");
     __device__ uint32_t raw_bar(int s) const { return bars + (uint32_t)sizeof(MxBars) + (uint32_t)s * 8u; }
     __device__ uint32_t x_empty_bar(int q) const { return raw_bar(kMaxStages + q); }
     __device__ uint32_t x_stage(int q) const { return smem + (uint32_t)(R * kWgStage + q * kWgXStage); }
@@ -191,6 +193,7 @@ struct RingAt {
 };
 
 struct WgradSmall : WgradCta<6, 4> {
+    static_assert(kX % kWgTeams == 0, "an X stage belongs to one team");
     static_assert(kRings >= (128 + 8) * kWgBN * 4, "the rings have room for a tile of partial sums");
     int64_t n0, k0;
     float *dw;
@@ -292,7 +295,6 @@ struct WgradSmall : WgradCta<6, 4> {
                 // The X stage first: its MMA, of step it - kX, comes behind that of step it - kRaw, whose phase of the raw barrier, another
                 // team's to wait for, is complete then.  A barrier tells a phase from the next only, so that before it a wait for this step's
                 // would return at once.
-                static_assert(kX <= kRaw, "the X stage's last step is not older than the raw stage's");
                 if (it >= kX) mbar_wait_warp(lane == 0 ? 1u : 0u, x_empty_bar(x.s), x.ph ^ 1u, abort_flag, g.status, g.wait_limit);
                 mbar_wait_warp(lane == 0 ? 1u : 0u, raw_bar(raw.s), raw.ph, abort_flag, g.status, g.wait_limit);
                 transform_stage(smem + (uint32_t)(raw.s * kWgStage), x_stage(x.s), place);
@@ -466,14 +468,18 @@ sparq_wgrad_small_kernel(const __grid_constant__ CUtensorMap map_dy, const __gri
 // columns of a row in registers.
 
 constexpr int kWgTile = 256;
-constexpr int kWgPairWorkers = 8;
+constexpr int kWgPairWorkers = 8, kWgPairTeams = kWgPairWorkers / 4;
 constexpr int kWgPairOwn = 128;                  // columns of a worker thread's row
 constexpr int kWgCodeWarp = 2;
 constexpr int kWgFirstWorker = 4;                // whole groups of four warps, for setmaxnreg
 constexpr int kWgPairThreads = 32 * (kWgFirstWorker + kWgPairWorkers);
 
 constexpr int kWgStages16 = 7;
-__host__ __device__ constexpr int wgrad_smem(bool x16) { return 1024 + (x16 ? kWgStages16 * 4 * kWgBox : WgradCta<7, 3>::kRings); }
+// Four X stages and six raw ones, multiples of the teams: a team waits for every phase of its own stages' barriers, and so for one that is no
+// more than one ahead of what it has seen.  (Seven and three: every other phase of a stage was the other team's, and a team took its word from
+// another barrier's arrival, which nothing orders.)
+using WgradPairRings = WgradCta<6, 4>;
+__host__ __device__ constexpr int wgrad_smem(bool x16) { return 1024 + (x16 ? kWgStages16 * 4 * kWgBox : WgradPairRings::kRings); }
 
 // The first `whole` tiles run over all tokens, the others (the tail) over the parts that the launch takes.  Where those follow whole tiles,
 // the first part's sums go to dw, the others' into tail_sums, 256 x 256 for each tile, or in launches of their own (skip: of the tail only)
@@ -514,7 +520,8 @@ struct WgradItem {
 // full: dy of both CTAs, in the leader; raw: codes and scales of this CTA; xf: transformed by both CTAs' workers,
 // in the leader; empty: the MMAs that read the stage have retired; acc, freed: as above.
 template <bool X16>
-struct WgradPair : WgradCta<7, 3> {
+struct WgradPair : WgradPairRings {
+    static_assert(kX % kWgPairTeams == 0 && kRaw % kWgPairTeams == 0, "a stage belongs to one team");
     static constexpr int kXAt = 2 * kWgBox, kStage = X16 ? kXAt + kWgXStage : kWgStage, kStages = X16 ? kWgStages16 : kRaw;
     int tiles, pair;
 
@@ -655,8 +662,7 @@ struct WgradPair : WgradCta<7, 3> {
             const int c_first = c;
             for (int b = 0; b < steps_of; ++b) {
                 if (!X16) {
-                    if ((stage & 1) == team) {
-                        // the X stage first, as above
+                    if (stage % kWgPairTeams == team) {
                         if (stage >= kX) mbar_wait_warp(lane == 0 ? 1u : 0u, x_empty_bar(x.s), x.ph ^ 1u, abort_flag, g.status, g.wait_limit);
                         mbar_wait_warp(lane == 0 ? 1u : 0u, raw_bar(raw.s), raw.ph, abort_flag, g.status, g.wait_limit);
                         transform_stage(smem + (uint32_t)(raw.s * kStage), x_stage(x.s), place);
