@@ -479,6 +479,13 @@ SPARQ_API int sparq_selftest_form(int n, int h, int w, int c, int cout, int r, i
                         int stride_h, int stride_w, int pad_h, int pad_w,
                         const sparq_params *p, int sms);
 
+/* Diagnostic: the form that sparq_wgrad_mx8 takes for these sizes on a device of `sms` multiprocessors, outside a stream
+ * capture or with a workspace.  Host arithmetic only: needs no device.  report, 6 words on the host: the kernel (0: tiles of
+ * 128 x 128; 1: pairs of CTAs, 256 x 256; 2: the same with X expanded to bf16 first), CTAs that share a tile, parts that the
+ * tokens are cut into, tiles, tiles that are not cut, and the bytes of scratch memory (sparq_wgrad_mx8_workspace_bytes).  The
+ * paper has no counterpart. */
+SPARQ_API int sparq_selftest_wgrad_form(int64_t M, int64_t N, int64_t K, int sms, int64_t *report);
+
 /* Text of the calling thread's most recent error ("" if none).  The pointer stays valid
  * until the thread's next failing call. */
 SPARQ_API const char *sparq_last_error(void);

@@ -25,15 +25,33 @@ struct WgradForm {
     int64_t tiles, whole;   // whole: tiles in front that are not cut into the parts
 };
 
+// X in bf16, and the sums of the parts: one piece of memory.
+struct Scratch {
+    size_t x, sums;
+    size_t bytes() const { return x + sums; }
+};
+Scratch scratch_of(const WgradForm &f, int64_t M, int64_t N, int64_t K)
+{
+    auto round = [](size_t b) { return (b + 255) / 256 * 256; };
+    return {f.expand ? round((size_t)M * (size_t)mx_padded(K) * 2) : 0,
+            f.parts == 1 ? 0
+            : f.whole ? (size_t)(f.parts - 1) * (size_t)(f.tiles - f.whole) * kWgTile * kWgTile * sizeof(float)
+                      : round((size_t)f.parts * (size_t)N * (size_t)K * sizeof(float))};
+}
+
 // By estimates of the time in us, fitted to launches of 64 to 100352 tokens and 64 x 256 to 2048 x 2048 outputs in every form: the choice is
 // within an eighth of the fastest.  A step of 64 tokens takes a tile 0.45 us (128 x 128, transformed on the way), 0.48 (256 x 256) and
 // 0.36 (256 x 256, expanded first).  16384 x 1024 x 1024: pairs in one part 128 us, in four 42, expanded first 89 and 40; 4096 x 128 x 1152: 128 x 128
-// 36 us, in eight parts 12.7, split in clusters of eight 11.5.
+// 36 us, in eight parts 12.7, split in clusters of eight 11.5.  A form whose scratch memory the library does not give (kWorkspaceMaxBytes) is none:
+// it would run as another, without it.
 WgradForm pick_wgrad(int64_t M, int64_t N, int64_t K, int blocks, int sms)
 {
     WgradForm best = {};
     double cost = 1e30;
     const bool x16_fits = (double)M * (double)mx_padded(K) * 2.0 <= (double)kWorkspaceMaxBytes;
+    auto consider = [&](double c, const WgradForm &f) {
+        if (c < cost - 0.05 && (!f.expand || x16_fits) && scratch_of(f, M, N, K).bytes() <= kWorkspaceMaxBytes) { cost = c; best = f; }
+    };
     const int64_t small = (N + 127) / 128 * ((K + 127) / 128), large = (N + 255) / 256 * ((K + 255) / 256);
     const double expand = 1.5 + (double)M * (double)K * 3.0 / 6.0e6;
     for (int parts = 1; parts <= 128 && parts * 8 <= blocks + 7; parts += parts < 8 ? 1 : parts < 32 ? 4 : 16) {
@@ -44,35 +62,22 @@ WgradForm pick_wgrad(int64_t M, int64_t N, int64_t K, int blocks, int sms)
         for (int split = 1; split <= 8 && split <= blocks / parts; split *= 2) {
             const int64_t at_once = clusters_at_once(split, sms), rounds = (small * parts + at_once - 1) / at_once;
             const double c = join + 1.0 + (double)rounds * (4.6 + 0.45 * ((b + split - 1) / split) + (split > 1 ? 1.5 : 0.0));
-            if (c < cost - 0.05) { cost = c; best = {false, false, split, parts, small, 0}; }
+            consider(c, {false, false, split, parts, small, 0});
         }
         const int64_t rounds = (large * parts + sms / 2 - 1) / (sms / 2);
-        const double q = join + 7.0 + (double)rounds * 0.48 * b, x = join + 7.0 + expand + (double)rounds * 0.36 * b;
-        if (q < cost - 0.05) { cost = q; best = {true, false, 1, parts, large, 0}; }
-        if (x < cost - 0.05 && x16_fits) { cost = x; best = {true, true, 1, parts, large, 0}; }
+        consider(join + 7.0 + (double)rounds * 0.48 * b, {true, false, 1, parts, large, 0});
+        consider(join + 7.0 + expand + (double)rounds * 0.36 * b, {true, true, 1, parts, large, 0});
     }
     // Whole tiles but for a last round that leaves most pairs without one, whose tiles are cut (256 tiles on 74 pairs: 3 rounds and
     // a half for 4; 16384 x 4096 x 4096 433 us, in two parts throughout 490; 4100 x 2560 x 2040 55 and 67).
     const int64_t pairs = sms / 2, tail = large % pairs;
     for (int parts = 2; parts <= 8 && parts * 8 <= blocks && large > pairs && tail > 0; ++parts) {
         const double b = (double)(large / pairs) * blocks + (double)((tail * parts + pairs - 1) / pairs) * ((blocks + parts - 1) / parts);
-        const double join = 3.0 + (double)(2 * parts * tail) * (kWgTile * kWgTile * 4.0 / 5.0e6), q = join + 7.0 + 0.48 * b, x = join + 7.0 + expand + 0.36 * b;
-        if (q < cost - 0.05) { cost = q; best = {true, false, 1, parts, large, large - tail}; }
-        if (x < cost - 0.05 && x16_fits) { cost = x; best = {true, true, 1, parts, large, large - tail}; }
+        const double join = 3.0 + (double)(2 * parts * tail) * (kWgTile * kWgTile * 4.0 / 5.0e6);
+        consider(join + 7.0 + 0.48 * b, {true, false, 1, parts, large, large - tail});
+        consider(join + 7.0 + expand + 0.36 * b, {true, true, 1, parts, large, large - tail});
     }
     return best;
-}
-
-struct Scratch {
-    size_t x, sums;
-};
-Scratch scratch_of(const WgradForm &f, int64_t M, int64_t N, int64_t K)
-{
-    auto round = [](size_t b) { return (b + 255) / 256 * 256; };
-    return {f.expand ? round((size_t)M * (size_t)mx_padded(K) * 2) : 0, 
-            f.parts == 1 ? 0
-            : f.whole ? (size_t)(f.parts - 1) * (size_t)(f.tiles - f.whole) * kWgTile * kWgTile * sizeof(float)
-                      : round((size_t)f.parts * (size_t)N * (size_t)K * sizeof(float))};
 }
 
 }  // namespace
@@ -89,8 +94,17 @@ extern "C" int64_t sparq_wgrad_mx8_workspace_bytes(int64_t M, int64_t N, int64_t
     int sms = 0;
     const int rc = device_info(&sms);
     if (rc != SPARQ_OK) return rc;
-    const Scratch need = scratch_of(pick_wgrad(M, N, K, (int)((M + kWgTokens - 1) / kWgTokens), sms), M, N, K);
-    return (int64_t)(need.x + need.sums);
+    return (int64_t)scratch_of(pick_wgrad(M, N, K, (int)((M + kWgTokens - 1) / kWgTokens), sms), M, N, K).bytes();
+}
+
+extern "C" int sparq_selftest_wgrad_form(int64_t M, int64_t N, int64_t K, int sms, int64_t *report)
+{
+    if (M < 1 || N < 1 || K < 1 || M >= kMxMost || N >= kMxMost || K >= kMxMost || sms < 1 || !report)
+        return set_error(SPARQ_ERR_INVALID_ARG, "bad sizes of a weight gradient");
+    const WgradForm f = pick_wgrad(M, N, K, (int)((M + kWgTokens - 1) / kWgTokens), sms);
+    const int64_t words[6] = {f.pairs ? f.expand ? 2 : 1 : 0, f.split, f.parts, f.tiles, f.whole, (int64_t)scratch_of(f, M, N, K).bytes()};
+    for (int i = 0; i < 6; ++i) report[i] = words[i];
+    return SPARQ_OK;
 }
 
 extern "C" int sparq_wgrad_mx8(const void *dy, int64_t lddy, const int8_t *codes, const uint8_t *scales,
@@ -133,15 +147,15 @@ extern "C" int sparq_wgrad_mx8(const void *dy, int64_t lddy, const int8_t *codes
     const WgradForm form = pick_wgrad(M, N, K, g.blocks, sms);
     const Scratch need = scratch_of(form, M, N, K);
     if (workspace && ((uintptr_t)workspace & 255u)) return set_error(SPARQ_ERR_UNSUPPORTED, "workspace must be 256-byte aligned");
-    if (workspace && workspace_bytes < need.x + need.sums)
-        return set_error(SPARQ_ERR_INVALID_ARG, "workspace of %zu bytes, %zu are needed", workspace_bytes, need.x + need.sums);
+    if (workspace && workspace_bytes < need.bytes())
+        return set_error(SPARQ_ERR_INVALID_ARG, "workspace of %zu bytes, %zu are needed", workspace_bytes, need.bytes());
     g.parts = form.parts;
     g.split = form.split;
     if (form.tiles * form.parts * form.split > INT64_C(1) << 30) return set_error(SPARQ_ERR_UNSUPPORTED, "more than 2^30 tiles");
     // Memory for X in bf16 and for the parts' sums: the caller's, else scratch.  Without any (a stream that is being captured) X is expanded
     // stage by stage and the parts add to dw one launch after the other: the same sums in the same order.
     CUtensorMap map_x;
-    const size_t bytes = need.x + need.sums;
+    const size_t bytes = need.bytes();
     void *const own = !workspace && bytes ? workspace_alloc(bytes, st) : nullptr;
     uint8_t *const room = (uint8_t *)(workspace ? workspace : own);
     void *const x = room && need.x ? room : nullptr;
