@@ -479,6 +479,11 @@ SPARQ_API int sparq_selftest_form(int n, int h, int w, int c, int cout, int r, i
                         int stride_h, int stride_w, int pad_h, int pad_w,
                         const sparq_params *p, int sms);
 
+/* Diagnostic: the form that sparq_gemm_mxf4 takes for these sizes on a device of `sms` multiprocessors.  Host arithmetic only:
+ * needs no device.  report, 3 words on the host: columns of a tile (16 or 32 rows of A beside 128 of B; 128 rows of B beside 128 of A;
+ * 256: pairs of CTAs, 256 x 256), CTAs that share a tile, tiles.  The paper has no counterpart. */
+SPARQ_API int sparq_selftest_mxf4_form(int64_t M, int64_t N, int64_t K, int sms, int64_t *report);
+
 /* Diagnostic: the form that sparq_wgrad_mx8 takes for these sizes on a device of `sms` multiprocessors, outside a stream
  * capture or with a workspace.  Host arithmetic only: needs no device.  report, 6 words on the host: the kernel (0: tiles of
  * 128 x 128; 1: pairs of CTAs, 256 x 256; 2: the same with X expanded to bf16 first), CTAs that share a tile, parts that the

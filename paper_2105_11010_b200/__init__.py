@@ -23,6 +23,6 @@ from ._binding import (  # noqa: F401
     sparq_mx_code_bytes, sparq_mx_scale_bytes, sparq_quantize_mx, sparq_dequantize_mx, sparq_gemm_mxf4,
     sparq_act_forward_mx8, sparq_act_backward_mx8, sparq_wgrad_mx8, sparq_wgrad_mx8_workspace_bytes,
     sparq_check, sparq_last_error, sparq_shutdown, sparq_selftest_wait_timeout, sparq_selftest_mma_rate, sparq_selftest_form,
-    sparq_selftest_wgrad_form,
+    sparq_selftest_mxf4_form, sparq_selftest_wgrad_form,
     FORM_FULL, FORM_SMALL, FORM_WINDOW_RESIDENT, FORM_WINDOW_STREAMED, FORM_TRANSFORM_FIRST,
 )

@@ -132,8 +132,8 @@ def load_library() -> ctypes.CDLL:
         L.sparq_selftest_mma_rate.restype = i32
         L.sparq_selftest_form.argtypes = [i32] * 11 + [ctypes.POINTER(_CParams), i32]
         L.sparq_selftest_form.restype = i32
-        L.sparq_selftest_wgrad_form.argtypes = [i64, i64, i64, i32, ctypes.POINTER(i64)]
-        L.sparq_selftest_wgrad_form.restype = i32
+        for f in (L.sparq_selftest_mxf4_form, L.sparq_selftest_wgrad_form):
+            f.argtypes, f.restype = [i64, i64, i64, i32, ctypes.POINTER(i64)], i32
         L.sparq_check.argtypes = [vp]
         L.sparq_check.restype = i32
         L.sparq_last_error.argtypes = []
@@ -232,6 +232,14 @@ def sparq_selftest_form(x_shape, w_shape, stride, pad, params: SparqParams, sms:
     if rc < 0:
         _raise(rc)
     return rc
+
+
+def sparq_selftest_mxf4_form(M: int, N: int, K: int, sms: int = 148) -> dict:
+    """The form that :func:`sparq_gemm_mxf4` takes for these sizes: ``columns`` of a tile (256: pairs of CTAs), ``split`` and ``tiles``;
+    host arithmetic only."""
+    report = (ctypes.c_int64 * 3)()
+    _raise(load_library().sparq_selftest_mxf4_form(int(M), int(N), int(K), int(sms), report))
+    return dict(zip(("columns", "split", "tiles"), report))
 
 
 def sparq_selftest_wgrad_form(M: int, N: int, K: int, sms: int = 148) -> dict:

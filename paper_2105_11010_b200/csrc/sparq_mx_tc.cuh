@@ -182,7 +182,7 @@ __device__ __forceinline__ void tc_mma_bf16_pair(uint32_t d_tmem, uint64_t adesc
 }
 
 // Clusters of 1, 2, 4 and 8 CTAs, one CTA on each SM, that run at once on an SM count like the B200's (148, 74, 33, 15: clusters stay
-// within a group of SMs).
+// within a group of SMs).  On a few SMs (a process may be given a share of them) 0 for sizes that do not fit.
 inline int clusters_at_once(int split, int sms) { return split == 1 ? sms : split == 2 ? sms / 2 : split == 4 ? sms * 33 / 148 : sms * 15 / 148; }
 
 // Barriers of a CTA, in shared memory.

@@ -65,10 +65,12 @@ Form pick_form(int64_t M, int64_t N, int k_blocks, int sms)
     const bool swap = M <= 32;
     const int bn = M <= 16 ? 16 : M <= 32 ? 32 : 128;
     Form best = {kPairTile, 1, pairs};
-    double cost = swap ? 1e30 : 3.2 + (double)((pairs + sms / 2 - 1) / (sms / 2)) * (1.5 + 0.28 * k_blocks);
+    double cost = swap || sms < 2 ? 1e30 : 3.2 + (double)((pairs + sms / 2 - 1) / (sms / 2)) * (1.5 + 0.28 * k_blocks);
     const int64_t tiles = (swap ? 1 : (M + 127) / 128) * n_tiles;
     for (int split = 1; split <= 8 && split <= k_blocks; split *= 2) {
-        const int64_t rounds = (tiles + clusters_at_once(split, sms) - 1) / clusters_at_once(split, sms);
+        const int64_t at_once = clusters_at_once(split, sms);
+        if (at_once == 0) break;
+        const int64_t rounds = (tiles + at_once - 1) / at_once;
         const int b = (k_blocks + split - 1) / split;
         double c = swap ? 1.95 + 0.26 * b : 3.1 + 0.3 * b;
         if (split > 1) c += swap ? 0.5 : 0.7 + 1.8 * (double)(M < 128 ? M : 128) / 128;
@@ -78,11 +80,26 @@ Form pick_form(int64_t M, int64_t N, int k_blocks, int sms)
     return best;
 }
 
+// 64-element MMAs of a reduction over K, and the steps that hold four of them.
+int mx_mmas(int64_t K) { return (int)((mx_padded(K) + 63) / 64); }
+int mx_steps(int64_t K) { return (mx_mmas(K) + kMxSteps - 1) / kMxSteps; }
+
 }  // namespace
 
 }  // namespace sparq
 
 using namespace sparq;
+
+extern "C" int sparq_selftest_mxf4_form(int64_t M, int64_t N, int64_t K, int sms, int64_t *report)
+{
+    if (M < 1 || N < 1 || K < 1 || M >= kMxMost || N >= kMxMost || K >= kMxMost || sms < 1 || !report)
+        return set_error(SPARQ_ERR_INVALID_ARG, "bad sizes of a product");
+    const Form f = pick_form(M, N, mx_steps(K), sms);
+    report[0] = f.bn;
+    report[1] = f.split;
+    report[2] = f.tiles;
+    return SPARQ_OK;
+}
 
 extern "C" int sparq_gemm_mxf4(const void *A, const uint8_t *A_scales, const void *B, const uint8_t *B_scales,
                                int64_t M, int64_t N, int64_t K, int format, const sparq_mx_epilogue *e, void *stream)
@@ -108,8 +125,8 @@ extern "C" int sparq_gemm_mxf4(const void *A, const uint8_t *A_scales, const voi
     MxGemmArgs g = {};
     g.M = M;
     g.N = N;
-    g.k_mmas = (int)((mx_padded(K) + 63) / 64);
-    g.k_blocks = (g.k_mmas + kMxSteps - 1) / kMxSteps;
+    g.k_mmas = mx_mmas(K);
+    g.k_blocks = mx_steps(K);
     g.scale_tiles = (int)(mx_scale_cols(format, K) / 4);
     g.a_scales = A_scales;
     g.b_scales = B_scales;

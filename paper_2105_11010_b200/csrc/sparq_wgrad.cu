@@ -52,7 +52,7 @@ WgradForm pick_wgrad(int64_t M, int64_t N, int64_t K, int blocks, int sms)
     auto consider = [&](double c, const WgradForm &f) {
         if (c < cost - 0.05 && (!f.expand || x16_fits) && scratch_of(f, M, N, K).bytes() <= kWorkspaceMaxBytes) { cost = c; best = f; }
     };
-    const int64_t small = (N + 127) / 128 * ((K + 127) / 128), large = (N + 255) / 256 * ((K + 255) / 256);
+    const int64_t small = (N + 127) / 128 * ((K + 127) / 128), large = (N + 255) / 256 * ((K + 255) / 256), pairs = sms / 2;
     const double expand = 1.5 + (double)M * (double)K * 3.0 / 6.0e6;
     for (int parts = 1; parts <= 128 && parts * 8 <= blocks + 7; parts += parts < 8 ? 1 : parts < 32 ? 4 : 16) {
         if (parts > 1 && (double)parts * (double)N * (double)K * 4.0 > (double)kWorkspaceMaxBytes) break;
@@ -60,17 +60,20 @@ WgradForm pick_wgrad(int64_t M, int64_t N, int64_t K, int blocks, int sms)
         const double join = parts > 1 ? 2.5 + (double)(parts + 1) * (double)N * (double)K * 4.0 / 5.0e6 : 0.0;
         // (the shorter parts have blocks / parts steps, and every CTA of a cluster needs one)
         for (int split = 1; split <= 8 && split <= blocks / parts; split *= 2) {
-            const int64_t at_once = clusters_at_once(split, sms), rounds = (small * parts + at_once - 1) / at_once;
+            const int64_t at_once = clusters_at_once(split, sms);
+            if (at_once == 0) break;
+            const int64_t rounds = (small * parts + at_once - 1) / at_once;
             const double c = join + 1.0 + (double)rounds * (4.6 + 0.45 * ((b + split - 1) / split) + (split > 1 ? 1.5 : 0.0));
             consider(c, {false, false, split, parts, small, 0});
         }
-        const int64_t rounds = (large * parts + sms / 2 - 1) / (sms / 2);
+        if (pairs == 0) continue;
+        const int64_t rounds = (large * parts + pairs - 1) / pairs;
         consider(join + 7.0 + (double)rounds * 0.48 * b, {true, false, 1, parts, large, 0});
         consider(join + 7.0 + expand + (double)rounds * 0.36 * b, {true, true, 1, parts, large, 0});
     }
     // Whole tiles but for a last round that leaves most pairs without one, whose tiles are cut (256 tiles on 74 pairs: 3 rounds and
     // a half for 4; 16384 x 4096 x 4096 433 us, in two parts throughout 490; 4100 x 2560 x 2040 55 and 67).
-    const int64_t pairs = sms / 2, tail = large % pairs;
+    const int64_t tail = pairs ? large % pairs : 0;
     for (int parts = 2; parts <= 8 && parts * 8 <= blocks && large > pairs && tail > 0; ++parts) {
         const double b = (double)(large / pairs) * blocks + (double)((tail * parts + pairs - 1) / pairs) * ((blocks + parts - 1) / parts);
         const double join = 3.0 + (double)(2 * parts * tail) * (kWgTile * kWgTile * 4.0 / 5.0e6);

@@ -41,3 +41,27 @@ def test_bad_sizes_are_refused():
         with pytest.raises(sparq.SparqError) as e:
             sparq.sparq_selftest_wgrad_form(*args)
         assert e.value.code == -1
+
+
+@pytest.mark.parametrize("sms", range(1, 161))
+def test_devices_of_few_multiprocessors(sms):
+    """A process may be given a share of a device: clusters that do not fit are not chosen, nor divided by."""
+    fits = {1: sms, 2: sms // 2, 4: sms // 4, 8: sms // 8}
+    for M in (1, 20, 100, 1000):
+        for N in (64, 4096):
+            for K in (64, 2048, 16384):
+                f = sparq.sparq_selftest_mxf4_form(M, N, K, sms)
+                assert fits[2 if f["columns"] == 256 else f["split"]] > 0, (M, N, K, f)
+                f = sparq.sparq_selftest_wgrad_form(K, N, M, sms)
+                assert fits[2 if f["kernel"] else f["split"]] > 0, (M, N, K, f)
+
+
+def test_forms_of_products():
+    """Rows of A in columns up to 32 of them, and pairs for large grids."""
+    assert sparq.sparq_selftest_mxf4_form(1, 4096, 4096)["columns"] == 16
+    assert sparq.sparq_selftest_mxf4_form(17, 4096, 4096)["columns"] == 32
+    assert sparq.sparq_selftest_mxf4_form(16384, 4096, 4096) == {"columns": 256, "split": 1, "tiles": 64 * 16}
+    for args in ((0, 1, 1), (1, 1 << 31, 1), (1, 1, 1, 0)):
+        with pytest.raises(sparq.SparqError) as e:
+            sparq.sparq_selftest_mxf4_form(*args)
+        assert e.value.code == -1
