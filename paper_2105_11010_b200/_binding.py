@@ -238,7 +238,7 @@ def sparq_selftest_mxf4_form(M: int, N: int, K: int, sms: int = 148) -> dict:
     """The form that :func:`sparq_gemm_mxf4` takes for these sizes: ``columns`` of a tile (256: pairs of CTAs), ``split`` and ``tiles``;
     host arithmetic only."""
     report = (ctypes.c_int64 * 3)()
-    _raise(load_library().sparq_selftest_mxf4_form(int(M), int(N), int(K), int(sms), report))
+    _raise(load_library().sparq_selftest_mxf4_form(_whole(M, "M"), _whole(N, "N"), _whole(K, "K"), _whole(sms, "sms", 32), report))
     return dict(zip(("columns", "split", "tiles"), report))
 
 
@@ -246,7 +246,7 @@ def sparq_selftest_wgrad_form(M: int, N: int, K: int, sms: int = 148) -> dict:
     """The form that :func:`sparq_wgrad_mx8` takes for these sizes: ``kernel`` (0 tiles of 128 x 128, 1 pairs, 2 pairs with X expanded
     first), ``split``, ``parts``, ``tiles``, ``whole`` and ``scratch_bytes``; host arithmetic only."""
     report = (ctypes.c_int64 * 6)()
-    _raise(load_library().sparq_selftest_wgrad_form(int(M), int(N), int(K), int(sms), report))
+    _raise(load_library().sparq_selftest_wgrad_form(_whole(M, "M"), _whole(N, "N"), _whole(K, "K"), _whole(sms, "sms", 32), report))
     return dict(zip(("kernel", "split", "parts", "tiles", "whole", "scratch_bytes"), report))
 
 
@@ -392,10 +392,18 @@ FORMAT_MXFP4, FORMAT_NVFP4, FORMAT_MXINT8 = 0, 1, 2
 ACT_IDENTITY, ACT_RELU, ACT_SILU, ACT_GELU = 0, 1, 2, 3
 
 
+def _whole(value: int, name: str, bits: int = 64) -> int:
+    """``value`` for a C integer of ``bits`` bits, which ctypes would cut off."""
+    value = int(value)
+    if not -(1 << (bits - 1)) <= value < 1 << (bits - 1):
+        raise ValueError(f"{name} does not fit {bits} bits")
+    return value
+
+
 def sparq_mx_code_bytes(fmt: int, rows: int, cols: int) -> int:
     """Bytes of a tensor's codes: rows of round_up(cols, 32) elements (uint8 (rows, that / 2) for the
     4-bit formats, int8 (rows, that) for MXINT8)."""
-    rc = load_library().sparq_mx_code_bytes(int(fmt), int(rows), int(cols))
+    rc = load_library().sparq_mx_code_bytes(_whole(fmt, "fmt", 32), _whole(rows, "rows"), _whole(cols, "cols"))
     if rc < 0:
         _raise(int(rc))
     return int(rc)
@@ -403,7 +411,7 @@ def sparq_mx_code_bytes(fmt: int, rows: int, cols: int) -> int:
 
 def sparq_mx_scale_bytes(fmt: int, rows: int, cols: int) -> int:
     """Bytes of a tensor's scales, padding included (uint8)."""
-    rc = load_library().sparq_mx_scale_bytes(int(fmt), int(rows), int(cols))
+    rc = load_library().sparq_mx_scale_bytes(_whole(fmt, "fmt", 32), _whole(rows, "rows"), _whole(cols, "cols"))
     if rc < 0:
         _raise(int(rc))
     return int(rc)
@@ -458,7 +466,7 @@ def sparq_act_backward_mx8(dy: torch.Tensor, codes: torch.Tensor, scales: torch.
 
 def sparq_wgrad_mx8_workspace_bytes(M: int, N: int, K: int) -> int:
     """Bytes of a workspace for :func:`sparq_wgrad_mx8` of these sizes on the current device."""
-    rc = load_library().sparq_wgrad_mx8_workspace_bytes(int(M), int(N), int(K))
+    rc = load_library().sparq_wgrad_mx8_workspace_bytes(_whole(M, "M"), _whole(N, "N"), _whole(K, "K"))
     if rc < 0:
         _raise(int(rc))
     return int(rc)

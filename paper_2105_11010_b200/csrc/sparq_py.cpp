@@ -66,6 +66,13 @@ struct Args {
         if (v == -1 && PyErr_Occurred()) throw PyFail();
         return v;
     }
+    // a format or another choice: an integer that the C ABI takes in 32 bits
+    int choice(const char *name)
+    {
+        const int64_t v = integer();
+        if (v != (int)v) fail("%s does not fit 32 bits", name);
+        return (int)v;
+    }
     float real()
     {
         const double v = PyFloat_AsDouble(next());
@@ -493,7 +500,7 @@ PyObject *mx_codec_call(PyObject *const *args, Py_ssize_t nargs, bool encode)
         Args a(args, nargs, 6);
         const char *name = encode ? "x" : "out";
         const Tensor &x = a.tensor(name);
-        const int format = (int)a.integer();
+        const int format = a.choice("fmt");
         const Tensor &c = a.tensor("codes"), &s = a.tensor("scales"), *m = a.opt("max_dev");
         int dt;
         int64_t ld;
@@ -518,7 +525,7 @@ SPARQ_PY(py_gemm_mxf4)
     return guarded([&] {
         Args a(args, nargs, 12);
         const Tensor &A = a.tensor("A"), &As = a.tensor("A_scales"), &B = a.tensor("B"), &Bs = a.tensor("B_scales");
-        const int format = (int)a.integer();
+        const int format = a.choice("fmt");
         if (A.dim() != 2 || B.dim() != 2) fail("%s must be matrices", "A and B");
         const int64_t M = A.size(0), N = B.size(0), K = 2 * A.size(1);
         if (2 * B.size(1) != K) fail("%s disagree on K", "A and B");
@@ -551,7 +558,7 @@ SPARQ_PY(py_act_forward_mx8)
     return guarded([&] {
         Args a(args, nargs, 9);
         const Tensor &x = a.tensor("x");
-        const int act = (int)a.integer();
+        const int act = a.choice("act");
         const Tensor &y = a.tensor("y"), &c = a.tensor("codes"), &s = a.tensor("scales");
         const Tensor *up = a.opt("up"), *uc = a.opt("up_codes"), *us = a.opt("up_scales");
         int dt;
@@ -574,7 +581,7 @@ SPARQ_PY(py_act_backward_mx8)
     return guarded([&] {
         Args a(args, nargs, 9);
         const Tensor &dy = a.tensor("dy");
-        const int act = (int)a.integer();
+        const int act = a.choice("act");
         const Tensor &c = a.tensor("codes"), &s = a.tensor("scales"), &dx = a.tensor("dx");
         const Tensor *uc = a.opt("up_codes"), *us = a.opt("up_scales"), *dup = a.opt("dup");
         int dt;
