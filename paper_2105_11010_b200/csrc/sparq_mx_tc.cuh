@@ -106,26 +106,63 @@ __device__ __forceinline__ bool mbar_try_wait_of(uint32_t mine, uint32_t bar, ui
     __syncwarp();
     return any;
 }
-__device__ __forceinline__ void mbar_wait_warp(uint32_t mine, uint32_t bar, uint32_t parity, volatile uint32_t *abort_flag, unsigned int *status,
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t mine, uint32_t bar, uint32_t parity, volatile uint32_t *abort_flag, unsigned int *status,
                                                long long limit_cycles)
 {
-    if (mbar_try_wait_of(mine, bar, parity)) return;
-    if (__any_sync(0xFFFFFFFFu, *abort_flag != 0u)) return;
+    if (mbar_try_wait_of(mine, bar, parity)) return true;
+    if (__any_sync(0xFFFFFFFFu, *abort_flag != 0u)) return false;
     const long long t0 = clock64();
     for (uint32_t it = 1;; ++it) {
-        if (mbar_try_wait_of(mine, bar, parity)) return;
+        if (mbar_try_wait_of(mine, bar, parity)) return true;
         if ((it & 0x3Fu) == 0) {
-            if (__any_sync(0xFFFFFFFFu, *abort_flag != 0u)) return;
+            if (__any_sync(0xFFFFFFFFu, *abort_flag != 0u)) return false;
             if (__any_sync(0xFFFFFFFFu, clock64() - t0 > limit_cycles)) {
                 if (mine) {
                     *abort_flag = 1u;
                     atomicOr(status, 1u);
                 }
                 __syncwarp();
-                return;
+                return false;
             }
         }
     }
+}
+
+// ---- after a wait that gave up -------------------------------------------------------------------------
+// No copy may land when its CTA has left.  So no stage is released that has not landed whole: an issuer or a team whose wait gave up stops, and
+// the producers come to a stand a ring behind the last release, at most.  Each says how many stages it issued, and what is on its way is
+// waited for.  Where several producers count on one barrier, a stage that only some of them came to would never complete: the issuer, if it
+// gave up, makes up for what the others owe it.  (One that did not give up has seen every stage land.  All of it behind the barrier at the
+// kernel's end: 0.1 us of every launch of a product.)
+constexpr uint32_t kStillIssuing = 0xFFFFFFFFu;
+
+// The last of `n` stages in a ring of S barriers from `bar` on, all of whose producers came to them.
+__device__ __forceinline__ void drain_ring(uint32_t bar, uint32_t S, uint32_t n, volatile uint32_t *abort_flag, unsigned int *status, long long limit)
+{
+#pragma unroll 1
+    for (uint32_t j = n > S ? n - S : 0; j < n; ++j) mbar_wait(bar + 8u * (j % S), j / S & 1u, abort_flag, status, limit, true);
+}
+// Stages of the producer that issued most; kStillIssuing if one has not stopped within the limit.
+__device__ __forceinline__ uint32_t most_issued(const volatile uint32_t *issued, int producers, long long limit)
+{
+    const long long t0 = clock64();
+    uint32_t n;
+    do {
+        n = 0;
+#pragma unroll 1
+        for (int p = 0; p < producers; ++p) n = issued[p] > n ? issued[p] : n;
+    } while (n == kStillIssuing && clock64() - t0 <= limit);
+    return n;
+}
+// Two producers of one CTA that both arrive on a stage's barrier.
+__device__ __forceinline__ void drain_two(uint32_t bar, uint32_t S, const volatile uint32_t *issued, volatile uint32_t *abort_flag, unsigned int *status,
+                                          long long limit)
+{
+    const uint32_t n = most_issued(issued, 2, limit);
+    if (n == kStillIssuing) return;
+#pragma unroll 1
+    for (uint32_t j = issued[0] < issued[1] ? issued[0] : issued[1]; j < n; ++j) mbar_arrive(bar + 8u * (j % S));
+    drain_ring(bar, S, n, abort_flag, status, limit);
 }
 
 // ---- CTA pairs (cta_group::2): one MMA over the operands and tensor memory of both ---------------------
@@ -148,6 +185,34 @@ __device__ __forceinline__ void tc_commit_pair(uint32_t bar, uint32_t elected)
     asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t"
                  "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n\t}"
                  :: "r"(bar), "h"((uint16_t)3), "r"(elected) : "memory");
+}
+// Four producers, two of each CTA, whose copies count on the leader's barriers: bytes 0 and 2 of a stage from producers 0 and 2 (one of each
+// CTA), bytes 1 from 1 and 3.  Producer 0, the leader's, announces a stage's bytes for all of them.
+__device__ __forceinline__ void mbar_complete_tx(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void drain_pair(uint32_t bar, uint32_t S, const volatile uint32_t *issued, uint32_t bytes0, uint32_t bytes1,
+                                           volatile uint32_t *abort_flag, unsigned int *status, long long limit)
+{
+    const uint32_t n = most_issued(issued, 4, limit);
+    if (n == kStillIssuing) return;
+#pragma unroll 1
+    for (uint32_t j = n > S ? n - S : 0; j < n; ++j) {
+        uint32_t on_way = 0;
+#pragma unroll 1
+        for (int p = 0; p < 4; ++p)
+            if (j < issued[p]) on_way += p & 1 ? bytes1 : bytes0;
+        const uint32_t at = bar + 8u * (j % S), owed = 2 * (bytes0 + bytes1) - on_way;
+        if (j >= issued[0]) mbar_expect_tx(at, on_way);
+        else if (owed) mbar_complete_tx(at, owed);
+        mbar_wait(at, j / S & 1u, abort_flag, status, limit, true);
+    }
+}
+// A word of another CTA of the cluster (an address from map_to_rank).
+__device__ __forceinline__ void store_remote(uint32_t dst, uint32_t v)
+{
+    asm volatile("st.shared::cluster.u32 [%0], %1;" :: "r"(dst), "r"(v) : "memory");
 }
 __device__ __forceinline__ void mbar_arrive_remote(uint32_t cluster_bar)
 {
@@ -193,7 +258,7 @@ struct MxBars {
 // One CTA's view of its work; the roles of its warps.
 struct MxCta {
     uint32_t smem, bars, tmem;          // operand ring (1024-byte aligned), MxBars, accumulator
-    volatile uint32_t *abort_flag;
+    volatile uint32_t *abort_flag, *issued;     // issued: stages of each producer that has stopped; in pairs the leader's words count
     int warp, lane, S, rank, steps;
     uint32_t split;
     __device__ uint32_t full_bar(int s) const { return bars + (uint32_t)s * 8u; }

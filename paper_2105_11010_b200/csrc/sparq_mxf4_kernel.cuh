@@ -64,15 +64,15 @@ struct Mxf4Pair : MxCta {
             if (CODES) dep_launch();
             const MxGemmArgs &g = p.g;
             const uint32_t leader_full = map_to_rank(full_bar(0), 0);
-            int s = 0, used = 0;
-            uint32_t ph = 1;
+            int s = 0;
+            uint32_t ph = 1, n = 0;
             bool live = true;
             for (int t = pair; t < tiles && live; t += p.pairs) {
                 int mt, nt;
                 pair_tile(p, t, mt, nt);
                 const int a_row = mt * kPairTile + rank * 128, b_row = nt * kPairTile + rank * 128;
                 for (int kb = 0; kb < g.k_blocks; ++kb) {
-                    if (used >= kStages && !mbar_wait(empty_bar(s), ph, abort_flag, g.status, g.wait_limit)) { live = false; break; }
+                    if (n >= kStages && !mbar_wait(empty_bar(s), ph, abort_flag, g.status, g.wait_limit)) { live = false; break; }
                     const uint32_t at = smem + (uint32_t)(s * kRoom), bar = leader_full + 8u * (uint32_t)s;
                     if (CODES) {
                         if (rank == 0) mbar_expect_tx(full_bar(s), 2 * kBytes);
@@ -82,19 +82,11 @@ struct Mxf4Pair : MxCta {
                         tma_load_pair_3d(at + kScalesAt, &map_a, bar, 0, kb * T, mt * 2 + rank);
                         tma_load_pair_3d(at + kScalesAt + T * kScaleTile, &map_b, bar, 0, kb * T, nt * 2);
                     }
-                    if (used < kStages) ++used;
+                    ++n;
                     if (++s == kStages) { s = 0; ph ^= 1u; }
                 }
             }
-            // After a wait that gave up no copy may land when the CTAs have left: the leader waits for what was announced (in vain, up
-            // to the limit, where another producer stopped earlier), the other CTA for the leader at the cluster's barrier.
-            if (CODES && *abort_flag && rank == 0) {
-                for (int j = 0; j < used; ++j) {
-                    const int q = s - 1 - j < 0 ? s - 1 - j + kStages : s - 1 - j;
-                    // ph is flipped whenever the ring starts over: the parity of the last phase announced on stage q
-                    mbar_wait(full_bar(q), q < s ? ph ^ 1u : ph, abort_flag, g.status, g.wait_limit, true);
-                }
-            }
+            store_remote(map_to_rank(smem_u32((const void *)(issued + 2 * rank + (CODES ? 0 : 1))), 0), n);
         }
         __syncwarp();
     }
@@ -106,11 +98,17 @@ struct Mxf4Pair : MxCta {
             const uint32_t elected = elect_one();
             int s = 0, i = 0;
             uint32_t ph = 0;
-            for (int t = pair; t < tiles; t += p.pairs, ++i) {
+            bool live = true;
+            for (int t = pair; t < tiles && live; t += p.pairs, ++i) {
                 const uint32_t d = tmem + (i & 1) * kPairSecond;
-                if (i > 0) mbar_wait_warp(elected, freed_bar(0), (uint32_t)(i - 1) & 1u, abort_flag, g.status, g.wait_limit);
+                if (i > 0) live = mbar_wait_warp(elected, freed_bar(0), (uint32_t)(i - 1) & 1u, abort_flag, g.status, g.wait_limit);
+                if (!live) break;
                 for (int kb = 0; kb < g.k_blocks; ++kb) {
-                    mbar_wait_warp(elected, full_bar(s), ph, abort_flag, g.status, g.wait_limit);
+                    live = mbar_wait_warp(elected, full_bar(s), ph, abort_flag, g.status, g.wait_limit);
+                    if (!live) {
+                        tc_commit_pair(acc_bar(i & 1), elected);        // what there is of the tile
+                        break;
+                    }
                     tc_fence_after();
                     const uint32_t at = smem + (uint32_t)(s * kRoom), sf = at + kScalesAt, ta = tmem + kPairScales, tb = ta + 4 * T;
                     const uint64_t adesc = make_smem_desc<kMxBK>(at), bdesc = make_smem_desc<kMxBK>(at + kHalf);
@@ -134,6 +132,10 @@ struct Mxf4Pair : MxCta {
             }
             // every MMA has retired before the warp goes on
             if (i > 0) mbar_wait(acc_bar((i - 1) & 1), (uint32_t)((i - 1) >> 1) & 1u, abort_flag, g.status, g.wait_limit, true);
+            if (!live && lane == 0) {
+                store_remote(map_to_rank(smem_u32((const void *)abort_flag), 1), 1u);        // the other CTA's producers stop, too
+                drain_pair(full_bar(0), kStages, issued, 2 * kHalf, 3 * T * kScaleTile, abort_flag, g.status, g.wait_limit);
+            }
         }
         __syncwarp();
     }
@@ -187,10 +189,12 @@ sparq_mxf4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     __shared__ __align__(8) MxBars bars;
     __shared__ uint32_t tmem_base_slot;
     __shared__ uint32_t abort_word;
+    __shared__ volatile uint32_t issued[4];
 
     Cta c;
     const int warp = c.warp = threadIdx.x >> 5, lane = c.lane = threadIdx.x & 31;
     c.abort_flag = &abort_word;
+    c.issued = issued;
     c.smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
     c.bars = smem_u32(&bars);
     c.rank = (int)(blockIdx.x & 1u);
@@ -211,6 +215,7 @@ sparq_mxf4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             mbar_init(c.acc_bar(1), 1);
             mbar_init(c.freed_bar(0), 2 * kPairEpiWarps);
             abort_word = 0;
+            for (int q = 0; q < 4; ++q) issued[q] = kStillIssuing;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
         __syncwarp();
@@ -231,7 +236,7 @@ sparq_mxf4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     case kPairScaleWarp: c.template produce<false>(map_sa, map_sb, p); break;
     default: c.finish(map_f, map_h, p);
     }
-    // Neither CTA leaves, or gives its tensor memory back, while the pair's MMAs or the other's arrivals may reach it.
+    // Neither CTA leaves, or gives its tensor memory back, while the pair's MMAs, the other's arrivals or a copy may reach it.
     tc_fence_before();
     __syncthreads();
     cluster_arrive();

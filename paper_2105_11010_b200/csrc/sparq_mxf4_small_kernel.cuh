@@ -201,9 +201,7 @@ struct Mxf4Small : MxCta {
                 tma_load_bytes(at + kScalesAt + (LANES ? 0 : T * kScaleTile), src + (int64_t)t0 * kScaleTile, sf, full);
                 if (++s == S) { s = 0; ph ^= 1u; }
             }
-            if (*abort_flag)       // none of this thread's copies may land after the CTA has exited
-                for (int j = it > S ? it - S : 0; j < it; ++j)
-                    mbar_wait(full_bar(j % S), (uint32_t)(j / S) & 1u, abort_flag, g.status, g.wait_limit, true);
+            issued[LANES ? 0 : 1] = (uint32_t)it;
         }
         __syncwarp();
     }
@@ -213,8 +211,9 @@ struct Mxf4Small : MxCta {
         const uint32_t elected = elect_one();
         int s = 0;
         uint32_t ph = 0;
+        bool live = true;
         for (int it = 0; it < steps; ++it) {
-            mbar_wait_warp(elected, full_bar(s), ph, abort_flag, g.status, g.wait_limit);
+            if (!mbar_wait_warp(elected, full_bar(s), ph, abort_flag, g.status, g.wait_limit)) { live = false; break; }
             tc_fence_after();
             const uint32_t at = smem + (uint32_t)(s * kStage), sf = at + kScalesAt;
             const int mmas = g.k_mmas - (kb_first + it) * kMxSteps;
@@ -235,6 +234,7 @@ struct Mxf4Small : MxCta {
         }
         tc_commit_if(acc_bar(), elected);
         mbar_wait(acc_bar(), 0, abort_flag, g.status, g.wait_limit, true);
+        if (!live && lane == 0) drain_two(full_bar(0), (uint32_t)S, issued, abort_flag, g.status, g.wait_limit);
         __syncwarp();
     }
 
@@ -379,10 +379,12 @@ sparq_mxf4_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_
     __shared__ __align__(8) MxBars bars;
     __shared__ uint32_t tmem_base_slot;
     __shared__ uint32_t abort_word;
+    __shared__ volatile uint32_t issued[2];
 
     Cta c;
     const int warp = c.warp = threadIdx.x >> 5, lane = c.lane = threadIdx.x & 31;
     c.abort_flag = &abort_word;
+    c.issued = issued;
     c.S = g.stages;
     c.smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
     c.bars = smem_u32(&bars);
@@ -413,6 +415,7 @@ sparq_mxf4_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_
             mbar_init(c.acc_bar(), 1);
             mbar_init(c.recv_bar(), 1);
             abort_word = 0;
+            issued[0] = issued[1] = kStillIssuing;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
         __syncwarp();

@@ -192,6 +192,12 @@ struct RingAt {
     __device__ void next() { if (++s == N) { s = 0; ph ^= 1u; } }
 };
 
+// drain_ring as a call: 64 x 512 x 512 4.78 us, inlined into WgradSmall's kernel 4.83.
+__device__ __noinline__ void drain_ring_call(uint32_t bar, uint32_t S, uint32_t n, volatile uint32_t *abort_flag, unsigned int *status, long long limit)
+{
+    drain_ring(bar, S, n, abort_flag, status, limit);
+}
+
 struct WgradSmall : WgradCta<6, 4> {
     static_assert(kX % kWgTeams == 0, "an X stage belongs to one team");
     static_assert(kRings >= (128 + 8) * kWgBN * 4, "the rings have room for a tile of partial sums");
@@ -209,7 +215,7 @@ struct WgradSmall : WgradCta<6, 4> {
             int it = 0, s = 0;
             uint32_t ph = 1;
             for (; it < steps; ++it) {
-                if (it >= S && !mbar_wait(empty_bar(s), ph, abort_flag, g.status, g.wait_limit)) break;
+                if (it >= S && !mbar_wait(empty_bar(s), ph, abort_flag, g.status, g.wait_limit)) { issued[DY ? 0 : 1] = (uint32_t)it; break; }
                 const uint32_t bar = DY ? full_bar(s) : raw_bar(s), at = smem + (uint32_t)(s * kWgStage);
                 const int m = (first + it) * kWgTokens;
                 mbar_expect_tx(bar, DY ? kWgCodes : kWgStage - kWgCodes);
@@ -222,9 +228,6 @@ struct WgradSmall : WgradCta<6, 4> {
                 }
                 if (++s == S) { s = 0; ph ^= 1u; }
             }
-            if (*abort_flag)       // none of this thread's copies may land after the CTA has exited
-                for (int j = it > S ? it - S : 0; j < it; ++j)
-                    mbar_wait(DY ? full_bar(j % S) : raw_bar(j % S), (uint32_t)(j / S) & 1u, abort_flag, g.status, g.wait_limit, true);
         }
         __syncwarp();
     }
@@ -239,9 +242,13 @@ struct WgradSmall : WgradCta<6, 4> {
         int c = 0;
         for (int it = 0; it < steps; ++it) {
             const int in = it & (kWgChunkSteps - 1);
-            if (in == 0 && c >= 2) mbar_wait_warp(elected, freed_bar(c & 1), (uint32_t)((c >> 1) - 1) & 1u, abort_flag, g.status, g.wait_limit);
-            mbar_wait_warp(elected, full_bar(raw.s), raw.ph, abort_flag, g.status, g.wait_limit);
-            mbar_wait_warp(elected, xf_bar(x.s), x.ph, abort_flag, g.status, g.wait_limit);
+            if (in == 0 && c >= 2 && !mbar_wait_warp(elected, freed_bar(c & 1), (uint32_t)((c >> 1) - 1) & 1u, abort_flag, g.status, g.wait_limit)) break;
+            if (!mbar_wait_warp(elected, full_bar(raw.s), raw.ph, abort_flag, g.status, g.wait_limit) ||
+                !mbar_wait_warp(elected, xf_bar(x.s), x.ph, abort_flag, g.status, g.wait_limit)) {
+                tc_commit_if(acc_bar(c & 1), elected);          // what there is of the chunk
+                ++c;
+                break;
+            }
             tc_fence_after();
             const bool chunk_ends = in == kWgChunkSteps - 1 || it == steps - 1;
             const uint32_t at = smem + (uint32_t)(raw.s * kWgStage), d = tmem + (uint32_t)((c & 1) * kWgBN);
@@ -295,8 +302,9 @@ struct WgradSmall : WgradCta<6, 4> {
                 // The X stage first: its MMA, of step it - kX, comes behind that of step it - kRaw, whose phase of the raw barrier, another
                 // team's to wait for, is complete then.  A barrier tells a phase from the next only, so that before it a wait for this step's
                 // would return at once.
-                if (it >= kX) mbar_wait_warp(lane == 0 ? 1u : 0u, x_empty_bar(x.s), x.ph ^ 1u, abort_flag, g.status, g.wait_limit);
-                mbar_wait_warp(lane == 0 ? 1u : 0u, raw_bar(raw.s), raw.ph, abort_flag, g.status, g.wait_limit);
+                // (A stage whose wait gave up is not handed on.)
+                if (it >= kX && !mbar_wait_warp(lane == 0 ? 1u : 0u, x_empty_bar(x.s), x.ph ^ 1u, abort_flag, g.status, g.wait_limit)) return;
+                if (!mbar_wait_warp(lane == 0 ? 1u : 0u, raw_bar(raw.s), raw.ph, abort_flag, g.status, g.wait_limit)) return;
                 transform_stage(smem + (uint32_t)(raw.s * kWgStage), x_stage(x.s), place);
                 fence_proxy_async_smem();
                 __syncwarp();
@@ -373,10 +381,12 @@ sparq_wgrad_small_kernel(const __grid_constant__ CUtensorMap map_dy, const __gri
     __shared__ __align__(8) WgradBars room;
     __shared__ uint32_t tmem_base_slot;
     __shared__ uint32_t abort_word;
+    __shared__ volatile uint32_t issued[2];
 
     WgradSmall c;
     const int warp = c.warp = threadIdx.x >> 5, lane = c.lane = threadIdx.x & 31;
     c.abort_flag = &abort_word;
+    c.issued = issued;
     c.S = WgradSmall::kRaw;
     c.smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
     c.bars = smem_u32(&room);
@@ -418,6 +428,7 @@ sparq_wgrad_small_kernel(const __grid_constant__ CUtensorMap map_dy, const __gri
             }
             mbar_init(c.recv_bar(), 1);
             abort_word = 0;
+            issued[0] = issued[1] = (uint32_t)c.steps;      // unless a producer stops in front of one
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
         __syncwarp();
@@ -441,6 +452,11 @@ sparq_wgrad_small_kernel(const __grid_constant__ CUtensorMap map_dy, const __gri
     // Every MMA of this CTA has retired (or a wait gave up), and none of its copies is on its way: the cluster's rings are
     // free for partial sums once all CTAs are here.
     __syncthreads();
+    if (threadIdx.x == 32 * (2 + kWgWorkers) && *c.abort_flag) {
+        drain_ring_call(c.full_bar(0), WgradSmall::kRaw, issued[0], c.abort_flag, g.status, g.wait_limit);
+        drain_ring_call(c.raw_bar(0), WgradSmall::kRaw, issued[1], c.abort_flag, g.status, g.wait_limit);
+    }
+    __syncwarp();
     if (split > 1) {
         cluster_arrive();
         cluster_wait();
@@ -532,14 +548,14 @@ struct WgradPair : WgradPairRings {
             if (DY) dep_launch();
             const WgradArgs &g = p.g;
             const uint32_t leader_full = map_to_rank(full_bar(0), 0);
-            int s = 0, used = 0;
-            uint32_t ph = 1;
+            int s = 0;
+            uint32_t ph = 1, done = 0;
             bool live = true;
             for (int t = pair; t < tiles && live; t += p.pairs) {
                 const WgradItem item(p, t);
                 const int n = item.nt * kWgTile + rank * 128, k = item.kt * kWgTile + rank * 128, sc = (k / 32) & ~15;
                 for (int b = item.first; b < item.last; ++b) {
-                    if (used >= kStages && !mbar_wait(empty_bar(s), ph, abort_flag, g.status, g.wait_limit)) { live = false; break; }
+                    if (done >= kStages && !mbar_wait(empty_bar(s), ph, abort_flag, g.status, g.wait_limit)) { live = false; break; }
                     const uint32_t at = smem + (uint32_t)(s * kStage);
                     const int m = b * kWgTokens;
                     if (DY) {
@@ -556,20 +572,13 @@ struct WgradPair : WgradPairRings {
                         tma_load_2d(at + kWgCodes, &map_a, raw_bar(s), k, m);
                         tma_load_2d(at + kWgScales, &map_b, raw_bar(s), sc, m);
                     }
-                    if (used < kStages) ++used;
+                    ++done;
                     if (++s == kStages) { s = 0; ph ^= 1u; }
                 }
             }
-            // After a wait that gave up no copy may land when the CTAs have left: each waits for the codes that it announced, the leader for
-            // both CTAs' dy (in vain, up to the limit, where the other producer stopped earlier), the other CTA for the leader at the
-            // cluster's barrier.
-            if (*abort_flag && (DY ? rank == 0 : !X16)) {
-                for (int j = 0; j < used; ++j) {
-                    const int q = s - 1 - j < 0 ? s - 1 - j + kStages : s - 1 - j;
-                    // ph is flipped whenever the ring starts over: the parity of the last phase announced on stage q
-                    mbar_wait(DY ? full_bar(q) : raw_bar(q), q < s ? ph ^ 1u : ph, abort_flag, g.status, g.wait_limit, true);
-                }
-            }
+            // (codes and scales count on their own CTA's barriers)
+            if (DY || X16) store_remote(map_to_rank(smem_u32((const void *)(issued + 2 * rank + (DY ? 0 : 1))), 0), done);
+            else issued[4] = done;
         }
         __syncwarp();
     }
@@ -584,14 +593,21 @@ struct WgradPair : WgradPairRings {
             RingAt<kStages> raw;
             RingAt<kX> x;
             int c = 0;
-            for (int t = pair; t < tiles; t += p.pairs) {
+            bool live = true;
+            for (int t = pair; t < tiles && live; t += p.pairs) {
                 const WgradItem item(p, t);
                 const int steps_of = item.last - item.first;
                 for (int b = 0; b < steps_of; ++b) {
                     const int in = b & (kWgChunkSteps - 1);
-                    if (in == 0 && c >= 2) mbar_wait_warp(elected, freed_bar(c & 1), (uint32_t)((c >> 1) - 1) & 1u, abort_flag, g.status, g.wait_limit);
-                    mbar_wait_warp(elected, full_bar(raw.s), raw.ph, abort_flag, g.status, g.wait_limit);
-                    if (!X16) mbar_wait_warp(elected, xf_bar(x.s), x.ph, abort_flag, g.status, g.wait_limit);
+                    if (in == 0 && c >= 2) live = mbar_wait_warp(elected, freed_bar(c & 1), (uint32_t)((c >> 1) - 1) & 1u, abort_flag, g.status, g.wait_limit);
+                    if (!live) break;
+                    live = mbar_wait_warp(elected, full_bar(raw.s), raw.ph, abort_flag, g.status, g.wait_limit) &&
+                           (X16 || mbar_wait_warp(elected, xf_bar(x.s), x.ph, abort_flag, g.status, g.wait_limit));
+                    if (!live) {
+                        tc_commit_pair(acc_bar(c & 1), elected);        // what there is of the chunk
+                        ++c;
+                        break;
+                    }
                     tc_fence_after();
                     const bool chunk_ends = in == kWgChunkSteps - 1 || b == steps_of - 1;
                     const uint32_t at = smem + (uint32_t)(raw.s * kStage), d = tmem + (uint32_t)((c & 1) * kWgTile);
@@ -609,6 +625,10 @@ struct WgradPair : WgradPairRings {
             }
             // every MMA has retired before the warp goes on
             if (c > 0) mbar_wait(acc_bar((c - 1) & 1), (uint32_t)((c - 1) >> 1) & 1u, abort_flag, g.status, g.wait_limit, true);
+            if (!live && lane == 0) {
+                store_remote(map_to_rank(smem_u32((const void *)abort_flag), 1), 1u);        // the other CTA's producers stop, too
+                drain_pair(full_bar(0), kStages, issued, 2 * kWgBox, X16 ? 2 * kWgBox : 0, abort_flag, g.status, g.wait_limit);
+            }
         }
         __syncwarp();
     }
@@ -663,8 +683,8 @@ struct WgradPair : WgradPairRings {
             for (int b = 0; b < steps_of; ++b) {
                 if (!X16) {
                     if (stage % kWgPairTeams == team) {
-                        if (stage >= kX) mbar_wait_warp(lane == 0 ? 1u : 0u, x_empty_bar(x.s), x.ph ^ 1u, abort_flag, g.status, g.wait_limit);
-                        mbar_wait_warp(lane == 0 ? 1u : 0u, raw_bar(raw.s), raw.ph, abort_flag, g.status, g.wait_limit);
+                        if (stage >= kX && !mbar_wait_warp(lane == 0 ? 1u : 0u, x_empty_bar(x.s), x.ph ^ 1u, abort_flag, g.status, g.wait_limit)) return;
+                        if (!mbar_wait_warp(lane == 0 ? 1u : 0u, raw_bar(raw.s), raw.ph, abort_flag, g.status, g.wait_limit)) return;
                         transform_stage(smem + (uint32_t)(raw.s * kStage), x_stage(x.s), place);
                         fence_proxy_async_smem();
                         __syncwarp();
@@ -696,11 +716,13 @@ sparq_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_cons
     __shared__ __align__(8) WgradBars room;
     __shared__ uint32_t tmem_base_slot;
     __shared__ uint32_t abort_word;
+    __shared__ volatile uint32_t issued[5];
 
     using Cta = WgradPair<X16>;
     Cta c;
     const int warp = c.warp = threadIdx.x >> 5, lane = c.lane = threadIdx.x & 31;
     c.abort_flag = &abort_word;
+    c.issued = issued;
     c.smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
     c.bars = smem_u32(&room);
     c.rank = (int)(blockIdx.x & 1u);
@@ -726,6 +748,7 @@ sparq_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_cons
                 mbar_init(c.freed_bar(b), 2 * kWgPairWorkers);
             }
             abort_word = 0;
+            for (int q = 0; q < 5; ++q) issued[q] = X16 || (q & 1) == 0 ? kStillIssuing : 0;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
         __syncwarp();
@@ -753,11 +776,13 @@ sparq_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_cons
         default: break;
         }
     }
-    // Neither CTA leaves, or gives its tensor memory back, while the pair's MMAs or the other's arrivals may reach it.
+    // Neither CTA leaves, or gives its tensor memory back, while the pair's MMAs, the other's arrivals or a copy may reach it.
     tc_fence_before();
     __syncthreads();
     cluster_arrive();
     cluster_wait();
+    // (The leader waited for the copies on its barriers.  Those of codes and scales are each CTA's own.)
+    if (!X16 && threadIdx.x == 32 * 3 && *c.abort_flag) drain_ring(c.raw_bar(0), Cta::kStages, issued[4], c.abort_flag, p.g.status, p.g.wait_limit);
     if (warp == 1) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" :: "r"(c.tmem), "r"(512u) : "memory");

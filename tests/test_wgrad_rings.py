@@ -45,7 +45,7 @@ def test_x_is_waited_for_before_codes():
     src = source()
     asked = re.findall(r"mbar_wait_warp\(lane == 0 \? 1u : 0u, (x_empty_bar\(x\.s\), x\.ph \^ 1u|raw_bar\(raw\.s\), raw\.ph),", src)
     assert [a.split("(")[0] for a in asked] == ["x_empty_bar", "raw_bar"] * 2
-    assert len(re.findall(r">= kX\) mbar_wait_warp\(lane == 0 \? 1u : 0u, x_empty_bar", src)) == 2
+    assert len(re.findall(r">= kX(?:\)| &&) !?mbar_wait_warp\(lane == 0 \? 1u : 0u, x_empty_bar", src)) == 2
 
 
 def model(raw, x, teams, seed, trials=2000):
