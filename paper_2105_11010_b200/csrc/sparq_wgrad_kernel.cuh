@@ -491,10 +491,12 @@ constexpr int kWgFirstWorker = 4;                // whole groups of four warps, 
 constexpr int kWgPairThreads = 32 * (kWgFirstWorker + kWgPairWorkers);
 
 constexpr int kWgStages16 = 7;
-// Four X stages and six raw ones, multiples of the teams: a team waits for every phase of its own stages' barriers, and so for one that is no
-// more than one ahead of what it has seen.  (Seven and three: every other phase of a stage was the other team's, and a team took its word from
-// another barrier's arrival, which nothing orders.)
-using WgradPairRings = WgradCta<6, 4>;
+// Three X stages are the teams' in turn, so that a barrier for each would hold every other phase for the other team, and a team could take a
+// phase for the one that it asks for only from another barrier's arrival, which nothing orders.  So there are two sets of them: step s
+// retires on barrier s % 6, which one team asks for, every phase of it.  (Six raw and four X stages, one set: 16384 x 1024 x 1024 in one
+// part 144 us instead of 139.)
+constexpr int kWgXSets = 2;
+using WgradPairRings = WgradCta<7, 3>;
 __host__ __device__ constexpr int wgrad_smem(bool x16) { return 1024 + (x16 ? kWgStages16 * 4 * kWgBox : WgradPairRings::kRings); }
 
 // The first `whole` tiles run over all tokens, the others (the tail) over the parts that the launch takes.  Where those follow whole tiles,
@@ -537,7 +539,8 @@ struct WgradItem {
 // in the leader; empty: the MMAs that read the stage have retired; acc, freed: as above.
 template <bool X16>
 struct WgradPair : WgradPairRings {
-    static_assert(kX % kWgPairTeams == 0 && kRaw % kWgPairTeams == 0, "a stage belongs to one team");
+    static constexpr int kXBars = kWgXSets * kX;
+    static_assert(kXBars % kWgPairTeams == 0 && kXBars <= kMaxStages, "a barrier belongs to one team");
     static constexpr int kXAt = 2 * kWgBox, kStage = X16 ? kXAt + kWgXStage : kWgStage, kStages = X16 ? kWgStages16 : kRaw;
     int tiles, pair;
 
@@ -592,6 +595,7 @@ struct WgradPair : WgradPairRings {
             constexpr uint32_t id = make_idesc_bf16_mn(kWgTile, 256);
             RingAt<kStages> raw;
             RingAt<kX> x;
+            RingAt<kXBars> xe;
             int c = 0;
             bool live = true;
             for (int t = pair; t < tiles && live; t += p.pairs) {
@@ -616,11 +620,12 @@ struct WgradPair : WgradPairRings {
                     for (int k = 0; k < kWgTokens / 16; ++k)
                         tc_mma_bf16_pair(d, adesc + (uint64_t)(k * 128), bdesc + (uint64_t)(k * 128), id, (in > 0 || k > 0) ? 1u : 0u, elected);
                     tc_commit_pair(empty_bar(raw.s), elected);
-                    if (!X16) tc_commit_pair(x_empty_bar(x.s), elected);
+                    if (!X16) tc_commit_pair(x_empty_bar(xe.s), elected);
                     if (chunk_ends) tc_commit_pair(acc_bar(c & 1), elected);
                     if (chunk_ends) ++c;
                     raw.next();
                     x.next();
+                    xe.next();
                 }
             }
             // every MMA has retired before the warp goes on
@@ -671,6 +676,7 @@ struct WgradPair : WgradPairRings {
         const uint32_t leader_xf = map_to_rank(xf_bar(0), 0), leader_freed = map_to_rank(freed_bar(0), 0);
         RingAt<kStages> raw;
         RingAt<kX> x;
+        RingAt<kXBars> xe;
         int c = 0, stage = 0;
         for (int t = pair; t < tiles; t += p.pairs) {
             const WgradItem item(p, t);
@@ -683,7 +689,8 @@ struct WgradPair : WgradPairRings {
             for (int b = 0; b < steps_of; ++b) {
                 if (!X16) {
                     if (stage % kWgPairTeams == team) {
-                        if (stage >= kX && !mbar_wait_warp(lane == 0 ? 1u : 0u, x_empty_bar(x.s), x.ph ^ 1u, abort_flag, g.status, g.wait_limit)) return;
+                        const bool wrap = xe.s < kX;            // step - kX: its barrier, and whether that lies in the round before
+                        if (stage >= kX && !mbar_wait_warp(lane == 0 ? 1u : 0u, x_empty_bar(wrap ? xe.s + kXBars - kX : xe.s - kX), wrap ? xe.ph ^ 1u : xe.ph, abort_flag, g.status, g.wait_limit)) return;
                         if (!mbar_wait_warp(lane == 0 ? 1u : 0u, raw_bar(raw.s), raw.ph, abort_flag, g.status, g.wait_limit)) return;
                         transform_stage(smem + (uint32_t)(raw.s * kStage), x_stage(x.s), place);
                         fence_proxy_async_smem();
@@ -693,6 +700,7 @@ struct WgradPair : WgradPairRings {
                     ++stage;
                     raw.next();
                     x.next();
+                    xe.next();
                 }
                 if ((b & (kWgChunkSteps - 1)) == kWgChunkSteps - 1 && b < steps_of - 1) {
                     if (c > c_first) add_chunk(g, c - 1, leader_freed, sum);
@@ -739,10 +747,8 @@ sparq_wgrad_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_cons
                 mbar_init(c.raw_bar(s), 1);
                 mbar_init(c.empty_bar(s), 1);
             }
-            for (int q = 0; q < Cta::kX; ++q) {
-                mbar_init(c.xf_bar(q), 2 * 4);         // a team of each CTA
-                mbar_init(c.x_empty_bar(q), 1);
-            }
+            for (int q = 0; q < Cta::kX; ++q) mbar_init(c.xf_bar(q), 2 * 4);         // a team of each CTA
+            for (int q = 0; q < Cta::kXBars; ++q) mbar_init(c.x_empty_bar(q), 1);
             for (int b = 0; b < 2; ++b) {
                 mbar_init(c.acc_bar(b), 1);
                 mbar_init(c.freed_bar(b), 2 * kWgPairWorkers);
