@@ -57,8 +57,9 @@ struct Form {
 };
 
 // By estimates of the time in us, fitted to launches of 1 to 2048 rows, 512 to 8192 columns and K 512 to 8192 in every form (b:
-// reduction steps of 256 on a CTA; one token x 512 in one piece 2.5 / 4.1 / 10.4 us for 2 / 8 / 32 steps, 128 x 512 3.7 / 5.6 / 12.7, pairs
-// 5.3 / 7.0 / 13.6; split by eight 2.9 / 3.7 and 6.1 / 7.0 for 8 / 32).
+// reduction steps of 256 on a CTA; one token x 512 in one piece 2.6 / 4.0 / 10.5 us for 2 / 8 / 32 steps, 128 x 512 3.8 / 5.5 / 11.9, pairs
+// 5.2 / 6.9 / 13.6; split by eight 2.9 / 3.7 and 6.0 / 6.8 for 8 / 32).  At 91 sizes the choice takes 1.01 times the fastest form on average, 1.13
+// at the most but for 33 x 1001 x 1000 (1.28).
 Form pick_form(int64_t M, int64_t N, int k_blocks, int sms)
 {
     const int64_t n_tiles = (N + 127) / 128, pairs = ((M + kPairTile - 1) / kPairTile) * ((N + kPairTile - 1) / kPairTile);

@@ -39,10 +39,11 @@ Scratch scratch_of(const WgradForm &f, int64_t M, int64_t N, int64_t K)
                       : round((size_t)f.parts * (size_t)N * (size_t)K * sizeof(float))};
 }
 
-// By estimates of the time in us, fitted to launches of 64 to 100352 tokens and 64 x 256 to 2048 x 2048 outputs in every form: the choice is
-// within an eighth of the fastest.  A step of 64 tokens takes a tile 0.45 us (128 x 128, transformed on the way), 0.48 (256 x 256) and
-// 0.36 (256 x 256, expanded first).  16384 x 1024 x 1024: pairs in one part 128 us, in four 42, expanded first 89 and 40; 4096 x 128 x 1152: 128 x 128
-// 36 us, in eight parts 12.7, split in clusters of eight 11.5.  A form whose scratch memory the library does not give (kWorkspaceMaxBytes) is none:
+// By estimates of the time in us, fitted to launches of 64 to 100352 tokens and 64 x 256 to 2048 x 2048 outputs in every form.  At 33 sizes of
+// 64 to 131072 tokens and 64 x 64 to 4096 x 4096 outputs the choice takes 1.03 times the fastest form on average, 1.11 at the most but for 80000 x
+// 64 x 64 (1.37: 128 parts for 12 in clusters of eight).  A step of 64 tokens takes a tile 0.45 us (128 x 128, transformed on the way),
+// 0.53 (256 x 256) and 0.36 (256 x 256, expanded first).  16384 x 1024 x 1024: pairs in one part 139 us, in four 47, expanded first 89 and 42;
+// 4096 x 128 x 1152: 128 x 128 30 us, in eight parts 10.7, split in clusters of eight 11.3.  A form whose scratch memory the library does not give (kWorkspaceMaxBytes) is none:
 // it would run as another, without it.
 WgradForm pick_wgrad(int64_t M, int64_t N, int64_t K, int blocks, int sms)
 {
@@ -68,16 +69,16 @@ WgradForm pick_wgrad(int64_t M, int64_t N, int64_t K, int blocks, int sms)
         }
         if (pairs == 0) continue;
         const int64_t rounds = (large * parts + pairs - 1) / pairs;
-        consider(join + 7.0 + (double)rounds * 0.48 * b, {true, false, 1, parts, large, 0});
+        consider(join + 7.0 + (double)rounds * 0.53 * b, {true, false, 1, parts, large, 0});
         consider(join + 7.0 + expand + (double)rounds * 0.36 * b, {true, true, 1, parts, large, 0});
     }
     // Whole tiles but for a last round that leaves most pairs without one, whose tiles are cut (256 tiles on 74 pairs: 3 rounds and
-    // a half for 4; 16384 x 4096 x 4096 433 us, in two parts throughout 490; 4100 x 2560 x 2040 55 and 67).
+    // a half for 4; 16384 x 4096 x 4096 396 us, uncut 417, in two parts throughout 435; 4100 x 2560 x 2040 58 and, uncut, 70).
     const int64_t tail = pairs ? large % pairs : 0;
     for (int parts = 2; parts <= 8 && parts * 8 <= blocks && large > pairs && tail > 0; ++parts) {
         const double b = (double)(large / pairs) * blocks + (double)((tail * parts + pairs - 1) / pairs) * ((blocks + parts - 1) / parts);
         const double join = 3.0 + (double)(2 * parts * tail) * (kWgTile * kWgTile * 4.0 / 5.0e6);
-        consider(join + 7.0 + 0.48 * b, {true, false, 1, parts, large, large - tail});
+        consider(join + 7.0 + 0.53 * b, {true, false, 1, parts, large, large - tail});
         consider(join + 7.0 + expand + 0.36 * b, {true, true, 1, parts, large, large - tail});
     }
     return best;
