@@ -476,8 +476,8 @@ def sparq_wgrad_mx8(dy: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
                     accumulate: bool = False, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """``dw (N, K) = dy^T @ X`` (``+ dw``) with ``dy`` (M, N) bfloat16 and X (M, K) kept as MXINT8.
 
-    ``workspace``: uint8, :func:`sparq_wgrad_mx8_workspace_bytes`; needed for speed only, and only where
-    the call is captured into a graph."""
+    ``workspace``: uint8, :func:`sparq_wgrad_mx8_workspace_bytes`; needed for speed only, where the call is captured into a
+    graph, or takes more than the 256 MB of scratch memory that the library keeps between synchronizations."""
     rc = _native.wgrad_mx8(dy, codes, scales, dw, accumulate, workspace, stream)
     if rc:
         _raise(rc)

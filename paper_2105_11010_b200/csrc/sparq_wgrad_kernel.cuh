@@ -474,12 +474,12 @@ sparq_wgrad_small_kernel(const __grid_constant__ CUtensorMap map_dy, const __gri
 // ---- many output tiles -----------------------------------------------------------------------------------
 // A persistent pair of CTAs walks tiles of 256 x 256: one MMA (cta_group::2) multiplies 256 columns of dy by 256 of X.  Each CTA
 // brings its 128 columns of dy, and brings and transforms its 128 columns of X: a value of X is transformed once per row of tiles
-// of 256, half as often as with one CTA by itself.  A step of 64 tokens takes 0.48 us: the chain from the codes' arrival
+// of 256, half as often as with one CTA by itself.  A step of 64 tokens takes 0.50 to 0.55 us: the chain from the codes' arrival
 // through the transform to the MMA, more than any pipe.
 // X16: X comes as bf16 (the library's own, expanded from the codes by the launch before) and goes from TMA to the MMA, 0.36 us a step;
-// the workers only add up.  Same operands, same order of sums, same bits.  16384 x 4096 x 4096 433 us call after call with
-// the expansion's 35 (457 with L2 emptied in between), 1.27 PFLOP/s in all, at the power cap; 8192 tokens, in whole tiles: 11 TB/s of operands
-// from L2, tensor pipe 72 % active (four rounds for 3.46).
+// the workers only add up.  Same operands, same order of sums, same bits.  16384 x 4096 x 4096 396 to 450 us call after call with
+// the expansion's 35 (452 with L2 emptied in between), 1.2 to 1.39 PFLOP/s in all, at the power cap; 8192 tokens: 12 TB/s of operands
+// from L2, tensor pipe 81 % active.
 // Warps: 0 producer of dy, 2 of codes and scales, 1 tensor memory and (leader) MMA issue, 4..11 workers, each thread with 128
 // columns of a row in registers.
 
