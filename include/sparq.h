@@ -398,8 +398,8 @@ SPARQ_API int sparq_act_backward_mx8(const void *dy, int dtype, int64_t rows, in
  * workspace: DEVICE memory of sparq_wgrad_mx8_workspace_bytes, 256-byte aligned, the caller's until the work
  * ends; or NULL, and the call takes scratch memory as the fused calls do.  While the stream is being captured
  * there is no scratch memory, and a call without a workspace is slower, up to many times for a long sum into a small
- * dw.  The library keeps 256 MB of scratch memory between synchronizations; where a call needs more, allocating it costs one behind each
- * synchronization 1 to 3 ms, which a workspace saves.  Same results, bit for bit.  Calls, and replays of graphs, that may overlap must not share a workspace. */
+ * dw.  The library keeps 256 MB of scratch memory between synchronizations; where a call needs more, the first behind each synchronization
+ * waits 1 to 13 ms for it (measured on two machines), which a workspace saves.  Same results, bit for bit.  Calls, and replays of graphs, that may overlap must not share a workspace. */
 SPARQ_API int sparq_wgrad_mx8(const void *dy, int64_t lddy, const int8_t *codes, const uint8_t *scales,
                     int64_t M, int64_t N, int64_t K, int accumulate, float *dw,
                     void *workspace, size_t workspace_bytes, void *stream);
