@@ -10,8 +10,8 @@
 // 8 bytes and a sixteenth forward and backward per element of a gated bf16 pair.  8192 x 8192, gated silu: forward 94.8 us (5.7 TB/s),
 // backward 99.4 (5.5), where a copy reaches 6.55; at 64 registers half of an SM's warps fit, and the arithmetic (a power of two and
 // a reciprocal an element, 2.8 instructions a cycle) takes most of the issue slots that the loads leave.  Both types with the arithmetic of
-// fp32's (Logistic): 101.6 and 123; fp32 tensors themselves 141 and 152 with it, 140 and 143.5 with that of bf16's, rows of odd length
-// 4 to 8 % more.
+// fp32's (Logistic): 101.6 and 123, before it took its power of two as it does now; fp32 tensors themselves 141 and 143 with it, 140 and 142
+// with that of bf16's, rows of odd length 2 to 7 % more.
 #include "sparq_mx.cuh"
 
 namespace sparq {
@@ -20,6 +20,7 @@ namespace {
 
 constexpr float kGeluScale = 1.5957691216057308f;      // 2 sqrt(2 / pi)
 constexpr float kGeluCubic = 0.044715f;
+constexpr float kHalfLog2e = 0.72134752044448170f, kHalfLog2eRest = 9.6298150e-9f;      // log2(e) / 2 in fp32, and what that leaves
 
 // The reciprocal of a normal number whose reciprocal is one, off by 1 unit of 2^-23.
 __device__ __forceinline__ float reciprocal(float v)
@@ -45,7 +46,12 @@ struct Logistic {
     bool below;
     __device__ explicit Logistic(float z)
     {
-        h = expf(-0.5f * fabsf(z));
+        // h = 2^(-w log2(e) / 2): the product's rounding and the constant's come back as a factor 1 + lo ln 2
+        const float w = fminf(fabsf(z), 256.0f), u = __fmul_rn(w, -kHalfLog2e);
+        const float lo = __fmaf_rn(w, -kHalfLog2eRest, __fmaf_rn(w, -kHalfLog2e, -u));
+        float p;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(p) : "f"(u));
+        h = __fmaf_rn(p, __fmul_rn(lo, 0.69314718055994531f), p);
         t = __fmul_rn(h, h);
         r = reciprocal(__fadd_rn(1.0f, t));
         below = z < 0.0f;
@@ -89,7 +95,7 @@ __device__ __forceinline__ void act_both(float x, float &y, float &d)
             const Logistic s(z);
             y = s.times(x);
             const float q = c * dz * s.r * s.r;           // the second term over t
-            d = s.below ? s.h * (s.h * (s.r + q)) : __fmaf_rn(s.t, q, s.r);
+            d = s.num * (s.num * __fmaf_rn(s.below ? 1.0f : s.t, q, s.r));
         }
     }
 }

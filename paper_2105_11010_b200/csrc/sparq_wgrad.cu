@@ -43,8 +43,8 @@ Scratch scratch_of(const WgradForm &f, int64_t M, int64_t N, int64_t K)
 // 64 to 131072 tokens and 64 x 64 to 4096 x 4096 outputs the choice takes 1.03 times the fastest form on average, 1.11 at the most but for 80000 x
 // 64 x 64 (1.37: 128 parts for 12 in clusters of eight).  A step of 64 tokens takes a tile 0.45 us (128 x 128, transformed on the way),
 // 0.53 (256 x 256) and 0.36 (256 x 256, expanded first).  16384 x 1024 x 1024: pairs in one part 139 us, in four 47, expanded first 89 and 42;
-// 4096 x 128 x 1152: 128 x 128 30 us, in eight parts 10.7, split in clusters of eight 11.3.  A form whose scratch memory the library does not give (kWorkspaceMaxBytes) is none:
-// it would run as another, without it.
+// 4096 x 128 x 1152: 128 x 128 30 us, in eight parts 10.7, split in clusters of eight 11.3.  A form whose scratch memory the library does not
+// give (kWorkspaceMaxBytes) is none: it would run as another, without it.
 WgradForm pick_wgrad(int64_t M, int64_t N, int64_t K, int blocks, int sms)
 {
     WgradForm best = {};
