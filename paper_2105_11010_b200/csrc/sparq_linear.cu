@@ -146,16 +146,22 @@ cudaError_t launch_lin_small(const LinForm &f, const LinArgs &g, cudaStream_t st
     return launch_overlapped_cluster(kernel, (int)(f.tiles * f.split), f.split, lin_small_threads(SWAP), smem, st, map_x, map_w, map_out, p);
 }
 
+template <bool W_KN, bool F32, bool KEEP, bool PIECES>
+cudaError_t launch_pairs(const LinArgs &g, cudaStream_t st, const CUtensorMap &map_x, const CUtensorMap &map_w, const CUtensorMap &map_out)
+{
+    static bool attr_set[64] = {};
+    return launch_big(sparq_linear_kernel<W_KN, F32, KEEP, PIECES>, attr_set, 2 * g.units, 2, lin_threads(PIECES), kLinSmem, st, map_x, map_w, map_out, g);
+}
+
 template <bool W_KN, bool F32, bool KEEP>
 cudaError_t launch_linear(const LinForm &f, const LinArgs &g, cudaStream_t st, const CUtensorMap &map_x, const CUtensorMap &map_w, const CUtensorMap &map_out)
 {
-    static bool attr_set[64] = {};
     switch (f.bn) {
     case 16: return launch_lin_small<16, true, W_KN, F32, KEEP>(f, g, st, map_x, map_w, map_out);
     case 32: return launch_lin_small<32, true, W_KN, F32, KEEP>(f, g, st, map_x, map_w, map_out);
     case 64: return launch_lin_small<64, true, W_KN, F32, KEEP>(f, g, st, map_x, map_w, map_out);
     case 128: return launch_lin_small<128, false, W_KN, F32, KEEP>(f, g, st, map_x, map_w, map_out);
-    default: return launch_big(sparq_linear_kernel<W_KN, F32, KEEP>, attr_set, 2 * g.units, 2, kLinThreads, kLinSmem, st, map_x, map_w, map_out, g);
+    default: return g.k_blocks > g.piece ? launch_pairs<W_KN, F32, KEEP, true>(g, st, map_x, map_w, map_out) : launch_pairs<W_KN, F32, KEEP, false>(g, st, map_x, map_w, map_out);
     }
 }
 template <bool W_KN>
@@ -222,6 +228,7 @@ extern "C" int sparq_linear(const void *x, int64_t ldx, const void *w, int64_t l
     g.N = N;
     g.k_mmas = (int)((K + 15) / 16);
     g.k_blocks = (int)((K + kLinBK - 1) / kLinBK);
+    g.piece = lin_piece(K, e->out_dtype == SPARQ_DTYPE_F32 || e->z_codes);
     g.offsets = offsets;
     g.groups = (int)groups;
     g.bf16 = dtype == SPARQ_DTYPE_BF16;

@@ -6,8 +6,8 @@
 //
 // 16384 x 4096 x 4096 bf16 340 to 354 us in runs of milliseconds (1.55 to 1.62 PFLOP/s, one library product 334 to 350), 404 under the power cap (401); with bias, GELU and
 // a residual 362 and 438: what bounds it there is the cap.  Short sums are bound by the epilogue, two warps a scheduler whose stalls are dependent
-// instructions and instruction fetches: 8192 x 4096 x 1024 47 us, with SiLU 49, with z kept as well 59.  (Sixteen epilogue warps, for which the ring gives up
-// a stage: 359 instead of 346, and z kept no faster.  One kernel for all outputs: 54 and 68.)
+// instructions and instruction fetches: 8192 x 4096 x 1024 50 us, with SiLU 53, with z kept as well, the sum in three pieces, 73.  (Sixteen epilogue warps, for which the ring gives up
+// a stage: 359 instead of 346, and z kept no faster.)
 #pragma once
 
 #include "sparq_act.cuh"
@@ -19,6 +19,7 @@ namespace sparq {
 struct LinArgs {
     int64_t M, N;
     int k_mmas, k_blocks;               // reduction steps of 16 and of 64
+    int piece;                          // steps of 64 whose sum tensor memory holds without rounding to nearest
     const int32_t *offsets;             // of experts' rows, or nullptr
     int groups;
     int bf16;                           // operands: bf16, else fp16
@@ -45,6 +46,54 @@ constexpr int kLinSteps = 4;
 __device__ __forceinline__ constexpr uint32_t make_idesc_16(int n, int m, uint32_t bf16, bool a_mn, bool b_mn)
 {
     return (1u << 4) | (bf16 << 7) | (bf16 << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+
+// ---- sums in pieces ------------------------------------------------------------------------------------
+// The tensor cores cut a running sum off where fp32 would round it, so that its error grows with the number of additions and has a sign.  A sum therefore runs over a piece of K in
+// tensor memory, and pieces are added rounded to nearest in the registers of the warps that need the sum, while the next piece runs in another accumulator.
+//
+// What a cut-off piece of P terms of mixed signs is off by grows with P, what an fp32 sum of K terms is off by with the root of K.  Sums that fp32 outputs or kept z show take pieces of 12 sqrt(K)
+// elements, 1024 at the most (terms of one sign lose up to P / 16 units of 2^-23): fp32 outputs are 1.0 to 1.5 times as far off as an fp32 product, z in 8 bits 1.0 to 1.3 times (K = 64 to 8192; in one piece
+// 1.2 to 9.5 and 1.0 to 3.4 times).  16-bit outputs show none of this: pieces of 8192, which lose 2^-14 at the most, a quarter of the least half step that they are rounded by
+// (fp16, 2^-12).
+inline int lin_piece(int64_t K, bool shown)
+{
+    if (!shown) return 8192 / kLinBK;
+    int p = 1;
+    while (p < 1024 / kLinBK && (int64_t)(p + 1) * (p + 1) * 256 <= 9 * K) ++p;        // (64 p = 12 sqrt(K))
+    return p;
+}
+
+// C columns of a lane, a multiple of 32, or 16, of the `pieces` pieces from the CTA's n-th on, added up: at(b, h) is where the columns from h on of accumulator b are, freed(b) hands b back.
+template <int C, class Cta, class At, class Freed>
+__device__ __forceinline__ void lin_add_pieces(const Cta &c, const LinArgs &g, int pieces, int &n, float (&sum)[C], const At &at, const Freed &freed)
+{
+    constexpr int kAtOnce = C < 32 ? 1 : C < 64 ? 2 : 4;       // loads of 16 columns in flight
+    auto piece = [&](auto first) {
+        mbar_wait(c.acc_bar(n & 1), (uint32_t)(n >> 1) & 1u, c.abort_flag, g.status, g.wait_limit);
+        __syncwarp();
+        tc_fence_after();
+#pragma unroll
+        for (int h = 0; h < C; h += 16 * kAtOnce) {
+            uint32_t v[kAtOnce][32];
+#pragma unroll
+            for (int q = 0; q < kAtOnce; ++q) tmem_ld_32x16_issue(at(n & 1, h + 16 * q), v[q]);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 16 * kAtOnce; ++j) {
+                const float p = __uint_as_float(v[j / 16][j % 16]);
+                sum[h + j] = decltype(first)::value ? p : __fadd_rn(sum[h + j], p);
+            }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (c.lane == 0) freed(n & 1);
+        __syncwarp();
+        ++n;
+    };
+    piece(std::true_type{});
+#pragma unroll 1
+    for (int p = 1; p < pieces; ++p) piece(std::false_type{});
 }
 
 // ---- tiles of experts' rows ----------------------------------------------------------------------------
@@ -443,12 +492,12 @@ __device__ __forceinline__ void lin_stage_f32(const LinArgs &g, float (&y)[32], 
     }
 }
 
-// 64 columns from n on of a warp's 32 rows from m on, `rows` of them the expert's, from tensor memory; `clipped`: those behind them are no
-// rows of the output.  `scales`: those of z's two blocks.  `done`: the last columns have been read.  (Half a box at a time, one copy of the code: with both halves in registers
+// 64 columns from n on of a warp's 32 rows from m on, `rows` of them the expert's; `clipped`: those behind them are no
+// rows of the output.  `scales`: those of z's two blocks.  `columns(q, v)`: sums of each half, q = 0 and then 1.  (Half a box at a time, one copy of the code: with both halves in registers
 // and all of it unrolled, a launch spent microseconds on instruction fetches.)
-template <bool F32, bool KEEP, class Done>
-__device__ __forceinline__ void lin_put_span(const CUtensorMap &map, const LinArgs &g, uint32_t taddr, uint32_t stage, int64_t m, int rows, bool clipped, int64_t n,
-                                             float bias0, float bias1, LinFetch<F32> &fetch, uint32_t &scales, Done done)
+template <bool F32, bool KEEP, class Columns>
+__device__ __forceinline__ void lin_put_span(const CUtensorMap &map, const LinArgs &g, uint32_t stage, int64_t m, int rows, bool clipped, int64_t n,
+                                             float bias0, float bias1, LinFetch<F32> &fetch, uint32_t &scales, const Columns &columns)
 {
     const int lane = threadIdx.x & 31;
     if (!F32) {
@@ -458,9 +507,7 @@ __device__ __forceinline__ void lin_put_span(const CUtensorMap &map, const LinAr
 #pragma unroll 1
     for (int q = 0; q < 2; ++q) {
         uint32_t v[32];
-        tmem_ld_32x32_issue(taddr + q * 32, v);
-        tmem_ld_wait();
-        if (q == 1) done();
+        columns(q, v);
         if (n + 32 * q >= g.N) continue;
         float y[32];
         uint32_t scale = 0u;
@@ -485,16 +532,23 @@ __device__ __forceinline__ void lin_put_span(const CUtensorMap &map, const LinAr
 
 // ---- pairs of CTAs -----------------------------------------------------------------------------------------
 // Warps: 0 producer of x, 10 of w, 1 tensor memory and (leader) MMA issue, 2..9 epilogue (lane quarter warp % 4, two spans of 64 columns).
+//
+// PIECES: the epilogue's warps (4..11; 2 is w's producer, 3 has nothing to do) add the pieces up in registers and go on from there, so that both accumulators are free for the next tile's
+// first pieces.  8192 x 4096 x 1024 with z kept 73 us (in one piece 63), fp32 out 75 (62): the third piece runs when the epilogue is over; 16384 x 4096 x 4096 371 (354) and 360 (356).  (The sum back
+// in tensor memory: one piece runs beside the epilogue, 96 us in place of 73.  Tiles of 256 x 128, two sums and two pieces in tensor memory, warps of their own for the adding: 91, and a sum of 16384 432 us in
+// place of 373.)
 
 constexpr int kLinTile = 256;
-constexpr int kLinEpiWarps = 8, kLinWeightWarp = 2 + kLinEpiWarps;
-constexpr int kLinThreads = 32 * (kLinWeightWarp + 1);
+constexpr int kLinEpiWarps = 8;
+__host__ __device__ constexpr int lin_first_epi(bool pieces) { return pieces ? 4 : 2; }        // (whole groups of four warps, for setmaxnreg)
+__host__ __device__ constexpr int lin_weight_warp(bool pieces) { return pieces ? 2 : 2 + kLinEpiWarps; }
+__host__ __device__ constexpr int lin_threads(bool pieces) { return 32 * (pieces ? 4 + kLinEpiWarps : 3 + kLinEpiWarps); }
 constexpr int kLinHalf = 128 * kLinBK * 2;      // one operand's bytes of a step in one CTA
 constexpr int kLinStage = 2 * kLinHalf, kLinStages = 6;
 constexpr int kLinSmem = 1024 + kLinStages * kLinStage + kLinEpiWarps * kMxStaging;
 
 // W_KN: w is K x N; its boxes are 64 reduction rows x 64 columns, two for a CTA's 128 columns.
-template <bool W_KN, bool F32, bool KEEP>
+template <bool W_KN, bool F32, bool KEEP, bool PIECES>
 struct LinPair : MxCta {
     int pair;
 
@@ -537,17 +591,25 @@ struct LinPair : MxCta {
     {
         if (rank == 0) {
             const uint32_t elected = elect_one(), id = make_idesc_16(kLinTile, 256, (uint32_t)g.bf16, false, W_KN);
-            int s = 0, i = 0;
+            int s = 0, i = 0;           // tiles, or pieces counted through all tiles: the i-th adds up in accumulator i & 1
             uint32_t ph = 0;
             bool live = true;
             LinWalk<kLinTile> walk(g, lane);
             LinTile tile;
             for (uint32_t t = (uint32_t)pair; live && walk.find(t, tile); t += (uint32_t)g.units, ++i) {
-                const uint32_t d = tmem + (uint32_t)((i & 1) * kLinTile);
+                uint32_t d = tmem + (uint32_t)((i & 1) * kLinTile);
+                int in = 0;             // steps of the piece
                 if (i > 1) live = mbar_wait_warp(elected, freed_bar(i & 1), (uint32_t)((i >> 1) - 1) & 1u, abort_flag, g.status, g.wait_limit);
                 if (!live) break;
-                for (int kb = 0; kb < g.k_blocks; ++kb) {
-                    live = mbar_wait_warp(elected, full_bar(s), ph, abort_flag, g.status, g.wait_limit);
+                for (int kb = 0; kb < g.k_blocks; ++kb, ++in) {
+                    if (PIECES && in == g.piece) {
+                        tc_commit_pair(acc_bar(i & 1), elected);
+                        ++i;
+                        in = 0;
+                        d = tmem + (uint32_t)((i & 1) * kLinTile);
+                        if (i > 1) live = mbar_wait_warp(elected, freed_bar(i & 1), (uint32_t)((i >> 1) - 1) & 1u, abort_flag, g.status, g.wait_limit);
+                    }
+                    if (live) live = mbar_wait_warp(elected, full_bar(s), ph, abort_flag, g.status, g.wait_limit);
                     if (!live) {
                         tc_commit_pair(acc_bar(i & 1), elected);        // what there is of the tile
                         break;
@@ -560,7 +622,7 @@ struct LinPair : MxCta {
 #pragma unroll
                     for (int k = 0; k < kLinSteps; ++k) {
                         if (k >= mmas) continue;
-                        tc_mma_bf16_pair(d, adesc + (uint64_t)(k * 2), bdesc + (uint64_t)(k * (W_KN ? 128 : 2)), id, (kb > 0 || k > 0) ? 1u : 0u, elected);
+                        tc_mma_bf16_pair(d, adesc + (uint64_t)(k * 2), bdesc + (uint64_t)(k * (W_KN ? 128 : 2)), id, (in > 0 || k > 0) ? 1u : 0u, elected);
                     }
                     tc_commit_pair(empty_bar(s), elected);
                     if (kb == g.k_blocks - 1) tc_commit_pair(acc_bar(i & 1), elected);
@@ -581,8 +643,11 @@ struct LinPair : MxCta {
 
     __device__ void finish(const CUtensorMap &map, const LinArgs &g) const
     {
-        const int quarter = warp & 3, half = (warp - 2) >> 2;
-        const uint32_t freed = map_to_rank(freed_bar(0), 0), stage = smem + (uint32_t)(kLinStages * kLinStage + (warp - 2) * kMxStaging);
+        constexpr int kFirst = lin_first_epi(PIECES);
+        const int quarter = warp & 3, half = (warp - kFirst) >> 2, pieces = PIECES ? (g.k_blocks + g.piece - 1) / g.piece : 1;
+        const uint32_t freed = map_to_rank(freed_bar(0), 0), stage = smem + (uint32_t)(kLinStages * kLinStage + (warp - kFirst) * kMxStaging);
+        const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * 128);
+        const auto free_one = [&](int b) { mbar_arrive_remote(freed + 8u * (uint32_t)b); };
         const bool ahead = !F32 && g.residual;
         LinWalk<kLinTile> walk(g, lane);
         LinTile tile;
@@ -590,30 +655,45 @@ struct LinPair : MxCta {
         for (uint32_t t = (uint32_t)pair; walk.find(t, tile); t += (uint32_t)g.units, ++i) {
             const int64_t m = tile.m0 + rank * 128 + quarter * 32, n0 = (int64_t)tile.nt * kLinTile + half * 128;
             const int rows = tile.end - m < 0 ? 0 : tile.end - m < 32 ? (int)(tile.end - m) : 32;
+            float sum[PIECES ? 128 : 1];
+            if constexpr (PIECES) {
+                lin_add_pieces(*this, g, pieces, i, sum, [&](int b, int h) { return lanes + (uint32_t)(b * kLinTile + h); }, free_one);
+                --i;
+                if (rows == 0 || n0 >= g.N) continue;        // nothing of the warp's is an expert's
+            }
             float bias[4];
 #pragma unroll
             for (int q = 0; q < 4; ++q) bias[q] = lin_bias(g, tile.e, n0 + 32 * q);
             LinFetch<F32> fetch;
             if (ahead) fetch.issue(g, m, rows, n0, g.N);
-            mbar_wait(acc_bar(i & 1), (uint32_t)(i >> 1) & 1u, abort_flag, g.status, g.wait_limit);
+            if (!PIECES) mbar_wait(acc_bar(i & 1), (uint32_t)(i >> 1) & 1u, abort_flag, g.status, g.wait_limit);
             tc_fence_after();
-            if (rows == 0 || n0 >= g.N) {       // nothing of the warp's is an expert's
+            if (!PIECES && (rows == 0 || n0 >= g.N)) {       // nothing of the warp's is an expert's
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive_remote(freed + 8u * (uint32_t)(i & 1));
+                if (lane == 0) free_one(i & 1);
                 continue;
             }
-            const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)((i & 1) * kLinTile + half * 128);
+            const uint32_t taddr = lanes + (uint32_t)((i & 1) * kLinTile);
             uint32_t scales = 0u;
-#pragma unroll 1
+#pragma unroll (PIECES ? 2 : 1)
             for (int q = 0; q < 2; ++q) {
                 const int64_t n = n0 + q * 64;
                 uint32_t two = 0u;
-                lin_put_span<F32, KEEP>(map, g, taddr + q * 64, stage, m, rows, tile.end == g.M, n, bias[0], bias[1], fetch, two, [&] {
-                    if (q == 0) return;
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_remote(freed + 8u * (uint32_t)(i & 1));
+                lin_put_span<F32, KEEP>(map, g, stage, m, rows, tile.end == g.M, n, bias[0], bias[1], fetch, two, [&](int h, uint32_t(&v)[32]) {
+                    if constexpr (PIECES) {         // (the columns behind move up: registers have no index)
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(sum[64 * q + j]);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) sum[64 * q + j] = sum[64 * q + j + 32];
+                    } else {
+                        tmem_ld_32x32_issue(taddr + q * 64 + h * 32, v);
+                        tmem_ld_wait();
+                        if (q == 0 || h == 0) return;
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) free_one(i & 1);
+                    }
                 });
                 if (KEEP) scales |= two << (16 * q);
                 bias[0] = bias[2];
@@ -628,8 +708,8 @@ struct LinPair : MxCta {
     }
 };
 
-template <bool W_KN, bool F32, bool KEEP>
-__global__ void __launch_bounds__(kLinThreads, 1)
+template <bool W_KN, bool F32, bool KEEP, bool PIECES>
+__global__ void __launch_bounds__(lin_threads(PIECES), 1)
 sparq_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_out, const LinArgs g)
 {
     extern __shared__ uint8_t smem_raw[];
@@ -638,7 +718,7 @@ sparq_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
     __shared__ uint32_t abort_word;
     __shared__ volatile uint32_t issued[4];
 
-    LinPair<W_KN, F32, KEEP> c;
+    LinPair<W_KN, F32, KEEP, PIECES> c;
     const int warp = c.warp = threadIdx.x >> 5, lane = c.lane = threadIdx.x & 31;
     c.abort_flag = &abort_word;
     c.issued = issued;
@@ -676,11 +756,19 @@ sparq_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
     tc_fence_after();
     c.tmem = tmem_base_slot;
     dep_wait();
-    switch (warp) {
-    case 0: c.template produce<true>(map_x, g); break;
-    case 1: c.issue(g); break;
-    case kLinWeightWarp: c.template produce<false>(map_w, g); break;
-    default: c.finish(map_out, g);
+    // Registers: with PIECES 384 threads were launched with 168 each; of the same 64512, the epilogue's take 224 and the first four warps 56.
+    if (PIECES && warp >= lin_first_epi(true)) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+        c.finish(map_out, g);
+    } else {
+        if (PIECES) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        switch (warp) {
+        case 0: c.template produce<true>(map_x, g); break;
+        case 1: c.issue(g); break;
+        case lin_weight_warp(PIECES): c.template produce<false>(map_w, g); break;
+        default:
+            if (!PIECES) c.finish(map_out, g);
+        }
     }
     // Neither CTA leaves, or gives its tensor memory back, while the pair's MMAs, the other's arrivals or a copy may reach it.
     tc_fence_before();

@@ -58,7 +58,7 @@ template <int BN, bool SWAP, bool W_KN, bool F32, bool KEEP>
 struct LinSmall : MxCta {
     static constexpr int kEpi = lin_small_epi(SWAP), kGroup = lin_group(SWAP);
     static constexpr int kStage = lin_small_stage(BN), kLaneBytes = 128 * kLinBK * 2;
-    static constexpr uint32_t kCols = tmem_columns(BN);
+    static constexpr uint32_t kCols = tmem_columns(2 * BN);         // two accumulators, for sums in pieces
     uint32_t recv;
     int64_t m0, end;            // first row and end of the expert's
     int e, n0, rows, cols, kb_first, own, own_valid;
@@ -96,10 +96,17 @@ struct LinSmall : MxCta {
     {
         constexpr bool kRowsMn = SWAP && W_KN, kColsMn = !SWAP && W_KN;
         const uint32_t elected = elect_one(), id = make_idesc_16(BN, 128, (uint32_t)g.bf16, kRowsMn, kColsMn);
-        int s = 0;
+        int s = 0, n = 0, in = 0;           // piece, and its steps; piece n adds up in accumulator n & 1
         uint32_t ph = 0;
         bool live = true;
-        for (int it = 0; it < steps; ++it) {
+        for (int it = 0; it < steps; ++it, ++in) {
+            if (in == g.piece) {
+                tc_commit_if(acc_bar(n & 1), elected);
+                ++n;
+                in = 0;
+                if (n > 1) live = mbar_wait_warp(elected, freed_bar(n & 1), (uint32_t)((n >> 1) - 1) & 1u, abort_flag, g.status, g.wait_limit);
+                if (!live) break;
+            }
             if (!mbar_wait_warp(elected, full_bar(s), ph, abort_flag, g.status, g.wait_limit)) { live = false; break; }
             tc_fence_after();
             const uint32_t at = smem + (uint32_t)(s * kStage);
@@ -109,13 +116,13 @@ struct LinSmall : MxCta {
 #pragma unroll
             for (int k = 0; k < kLinSteps; ++k) {
                 if (k >= mmas) continue;
-                tc_mma_bf16(tmem, rdesc + (uint64_t)(k * (kRowsMn ? 128 : 2)), cdesc + (uint64_t)(k * (kColsMn ? 128 : 2)), id, (it > 0 || k > 0) ? 1u : 0u, elected);
+                tc_mma_bf16(tmem + (uint32_t)((n & 1) * BN), rdesc + (uint64_t)(k * (kRowsMn ? 128 : 2)), cdesc + (uint64_t)(k * (kColsMn ? 128 : 2)), id, (in > 0 || k > 0) ? 1u : 0u, elected);
             }
             tc_commit_if(empty_bar(s), elected);
             if (++s == S) { s = 0; ph ^= 1u; }
         }
-        tc_commit_if(acc_bar(), elected);
-        mbar_wait(acc_bar(), 0, abort_flag, g.status, g.wait_limit, true);
+        tc_commit_if(acc_bar(n & 1), elected);
+        mbar_wait(acc_bar(n & 1), (uint32_t)(n >> 1) & 1u, abort_flag, g.status, g.wait_limit, true);
         if (!live && lane == 0) drain_two(full_bar(0), (uint32_t)S, issued, abort_flag, g.status, g.wait_limit);
         __syncwarp();
     }
@@ -183,13 +190,39 @@ struct LinSmall : MxCta {
         }
     }
 
+    // Sums in several pieces, of the columns that the warp reads in finish(): back into the first accumulator, whence they are taken as one piece is.  (No third one for them: where CTAs of several launches share an
+    // SM, one would wait for tensor memory while its cluster waits for it, and may wait for another cluster that waits likewise.)
+    __device__ __forceinline__ void add_pieces(const LinArgs &g, uint32_t taddr, int half) const
+    {
+        constexpr int C = SWAP ? BN : 64;
+        float sum[C];
+        int n = 0;
+        auto at = [&](int b, int h) { return taddr + (uint32_t)(b * BN + h + (SWAP ? 0 : split == 1 ? half * 64 : half * 32 + (h & 32))); };
+        lin_add_pieces(*this, g, (steps + g.piece - 1) / g.piece, n, sum, at, [&](int b) { mbar_arrive(freed_bar(b)); });
+#pragma unroll
+        for (int h = 0; h < C; h += 16) {
+            uint4 v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float *s = sum + h + 4 * j;
+                v[j] = make_uint4(__float_as_uint(s[0]), __float_as_uint(s[1]), __float_as_uint(s[2]), __float_as_uint(s[3]));
+            }
+            tmem_st_32x16(at(0, h), v);
+        }
+        tmem_st_wait();
+    }
+
     __device__ void finish(const CUtensorMap &map, const LinArgs &g) const
     {
         const int quarter = warp & 3, half = (warp - 2) >> 2, r = quarter * 32 + lane;
         const float lane_bias = SWAP && g.bias && r < rows ? __ldg(g.bias + e * g.N + n0 + r) : 0.0f;
-        mbar_wait(acc_bar(), 0, abort_flag, g.status, g.wait_limit);
-        tc_fence_after();
         const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16);
+        if (steps > g.piece) {
+            add_pieces(g, taddr, half);
+        } else {
+            mbar_wait(acc_bar(), 0, abort_flag, g.status, g.wait_limit);
+            tc_fence_after();
+        }
         if (split > 1) {
             __syncwarp();
             cluster_wait();        // every CTA of the cluster has its barriers ready
@@ -202,8 +235,11 @@ struct LinSmall : MxCta {
                     LinFetch<F32> fetch;
                     if (g.residual && !F32) fetch.issue(g, m, live, n, g.N);
                     uint32_t scales = 0u;
-                    lin_put_span<F32, KEEP>(map, g, taddr + half * 64, smem + (uint32_t)((warp - 2) * kMxStaging), m, live, end == g.M, n,
-                                            lin_bias(g, e, n), lin_bias(g, e, n + 32), fetch, scales, [] {});
+                    lin_put_span<F32, KEEP>(map, g, smem + (uint32_t)((warp - 2) * kMxStaging), m, live, end == g.M, n, lin_bias(g, e, n), lin_bias(g, e, n + 32), fetch, scales,
+                                            [&](int h, uint32_t(&v)[32]) {
+                                                tmem_ld_32x32_issue(taddr + half * 64 + h * 32, v);
+                                                tmem_ld_wait();
+                                            });
                     if (KEEP && lane < live) lin_keep_scales<2>(g, scales, m + lane, n);
                     if (lane == 0) tma_store_wait_all();
                     __syncwarp();
@@ -310,7 +346,10 @@ sparq_linear_small_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
                 mbar_init(c.full_bar(s), 2);
                 mbar_init(c.empty_bar(s), 1);
             }
-            mbar_init(c.acc_bar(), 1);
+            for (int b = 0; b < 2; ++b) {
+                mbar_init(c.acc_bar(b), 1);
+                mbar_init(c.freed_bar(b), Cta::kEpi);
+            }
             mbar_init(c.recv_bar(), 1);
             abort_word = 0;
             issued[0] = issued[1] = kStillIssuing;
