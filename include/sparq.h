@@ -440,7 +440,7 @@ typedef struct {
  * K is 1 or more; M == 0 or N == 0 is a no-op.  Sums are held in fp32 in an order that depends on the sizes only.  The tensor cores add 16 products at a
  * time and cut the running sum off where rounding would be to nearest; sums therefore run over pieces of P elements of K, which are added rounded to nearest: terms of one sign lose up to P / 16 units
  * of 2^-23.  With fp32 outputs or z kept P is 12 sqrt(K), 1024 at the most (fp32 outputs are off by 3e-7 at K = 1024 and 6e-7 at 4096, 2-norm, an fp32 product by 2e-7 and 5e-7); else it is
- * 8192, which 16 bits do not show (2^-14).
+ * 8192, which 16 bits do not show (2^-14).  A row's outputs are, to the last bit, a matter of that row and the weights: not of the rows beside it or of what lies where an expert has none.
  * Requirements (else SPARQ_ERR_UNSUPPORTED): x and w 16-byte aligned, ldx, ldw and w_stride multiples of 8 (ldx of a single row is not
  * looked at), out, residual and bias aligned to their elements, z_codes and z_scales to 16 bytes, M, N and K below 2^31 - 256. */
 SPARQ_API int sparq_linear(const void *x, int64_t ldx, const void *w, int64_t ldw, int64_t w_stride, int transposed, int dtype,

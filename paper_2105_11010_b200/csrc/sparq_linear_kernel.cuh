@@ -168,9 +168,9 @@ struct LinWalk {
 
 // ---- epilogue ----------------------------------------------------------------------------------------------
 
-// SILU and GELU of C values beside 16-bit outputs.  Powers of two and reciprocals share one unit, 16 lanes a cycle, which is what these functions wait for;
-// two reciprocals come from one: 1 / a = b / (a b).  That is in range for z above -43 (a = 1 + exp(-z) below 2^63); a warp that holds lesser ones, or NaN, which would go from one
-// to the other, takes the functions one by one.
+// SILU and GELU of C columns of a lane's row beside 16-bit outputs.  Powers of two and reciprocals share one unit, 16 lanes a cycle, which is what these functions wait for;
+// two reciprocals come from one: 1 / a = b / (a b).  That is in range for z above -43 (a = 1 + exp(-z) below 2^63); a lane that holds lesser ones, or NaN, which would go from one
+// to the other, takes the functions one by one.  (Each lane for itself: a row's bits depend on no other row, and on nothing that lies where there is none.)
 template <int ACT, int C>
 __device__ __forceinline__ void lin_logistic(float (&y)[C])
 {
@@ -179,42 +179,43 @@ __device__ __forceinline__ void lin_logistic(float (&y)[C])
 #pragma unroll
     for (int j = 0; j < C; j += 2) asm("min.NaN.f32 %0, %1, %2, %3;" : "=f"(least) : "f"(least), "f"(y[j]), "f"(y[j + 1]));
     // (gelu's argument is above -43 down to -7.5; both rise with y)
-    if (__any_sync(0xFFFFFFFFu, !(least >= (ACT == SPARQ_ACT_SILU ? -43.0f : -7.5f)))) {
+    if (!(least >= (ACT == SPARQ_ACT_SILU ? -43.0f : -7.5f))) {
 #pragma unroll
         for (int j = 0; j < C; ++j) y[j] = act_value<true, ACT>(y[j]);
-        return;
-    }
+    } else {
 #pragma unroll
-    for (int j = 0; j < C; j += 2) {
-        float a[2];
+        for (int j = 0; j < C; j += 2) {
+            float a[2];
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            float e;
-            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(__fmul_rn(act_argument<ACT>(y[j + q]), -1.4426950408889634f)));
-            a[q] = __fadd_rn(1.0f, e);
+            for (int q = 0; q < 2; ++q) {
+                float e;
+                asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(__fmul_rn(act_argument<ACT>(y[j + q]), -1.4426950408889634f)));
+                a[q] = __fadd_rn(1.0f, e);
+            }
+            const float r = reciprocal(__fmul_rn(a[0], a[1]));
+            y[j] = __fmul_rn(y[j], __fmul_rn(a[1], r));
+            y[j + 1] = __fmul_rn(y[j + 1], __fmul_rn(a[0], r));
         }
-        const float r = reciprocal(__fmul_rn(a[0], a[1]));
-        y[j] = __fmul_rn(y[j], __fmul_rn(a[1], r));
-        y[j + 1] = __fmul_rn(y[j + 1], __fmul_rn(a[0], r));
     }
+    __syncwarp();
 }
 
-// A warp's lanes call it together.
-template <bool FAST, int C>
+// A warp's lanes call it together.  ROW: the values are columns of one row (else rows of one column, and each is taken by itself).
+template <bool FAST, bool ROW, int C>
 __device__ __forceinline__ void lin_act(float (&y)[C], int act)
 {
     if (act == SPARQ_ACT_RELU) {
 #pragma unroll
         for (int j = 0; j < C; ++j) y[j] = act_value<FAST, SPARQ_ACT_RELU>(y[j]);
     } else if (act == SPARQ_ACT_SILU) {
-        if (FAST) {
+        if (FAST && ROW) {
             lin_logistic<SPARQ_ACT_SILU>(y);
         } else {
 #pragma unroll
             for (int j = 0; j < C; ++j) y[j] = act_value<FAST, SPARQ_ACT_SILU>(y[j]);
         }
     } else if (act == SPARQ_ACT_GELU) {
-        if (FAST) {
+        if (FAST && ROW) {
             lin_logistic<SPARQ_ACT_GELU>(y);
         } else {
 #pragma unroll
@@ -288,7 +289,7 @@ __device__ __forceinline__ void lin_value(const LinArgs &g, float (&y)[32], cons
         for (int j = 0; j < 32; ++j) y[j] = __fadd_rn(y[j], __shfl_sync(0xFFFFFFFFu, bias, j));
     }
     if (KEEP && live && n < g.N) scale = lin_keep(g, y, row, n);
-    lin_act<!F32>(y, g.act);
+    lin_act<!F32, true>(y, g.act);
 }
 
 // The residual of 32 rows x 128 bytes: read in whole vectors (of rows that start anywhere shifted into place), handed to each lane its row

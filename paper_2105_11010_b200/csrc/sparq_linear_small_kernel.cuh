@@ -157,7 +157,7 @@ struct LinSmall : MxCta {
                 for (int j = 0; j < kGroup; ++j)
                     if (j < count) lin_keep_across(g, y[j], first + j, n);
             }
-            lin_act<!F32>(y, g.act);
+            lin_act<!F32, false>(y, g.act);
 #pragma unroll
             for (int j = 0; j < kGroup; ++j) {
                 if (g.residual) y[j] = __fadd_rn(y[j], res[j]);
