@@ -422,7 +422,8 @@ SPARQ_API int64_t sparq_wgrad_mx8_workspace_bytes(int64_t M, int64_t N, int64_t 
 
 /* What happens to a product.  For output row m (of expert e) and column j, in fp32 and in this order:
  *     z = acc + bias[e][j];  y = act(z);  y = y + residual[m][j];  out[m][j] = y
- * act: SPARQ_ACT_*; beside 16-bit outputs SILU and GELU are off by less than 2^-14, beside fp32 ones by a few units of the last place. */
+ * act: SPARQ_ACT_*; beside 16-bit outputs SILU and GELU are off by less than 2^-14 (results below 2^-119 in magnitude may be 0), beside fp32 ones by a few units of the
+ * last place, down to the last subnormal. */
 typedef struct {
     const float *bias;         /* [N], or [groups][N] with offsets; device, or NULL */
     int32_t act;               /* SPARQ_ACT_* */

@@ -38,7 +38,17 @@ struct Logistic {
     {
         // h = 2^(-w log2(e) / 2): the product's rounding and the constant's come back as a factor 1 + lo ln 2
         const float w = fminf(fabsf(z), 256.0f), u = __fmul_rn(w, -kHalfLog2e);
+        take(z, u, __fmaf_rn(w, -kHalfLog2eRest, __fmaf_rn(w, -kHalfLog2e, -u)));
+    }
+    // s(z + rest), of |z| below 2^16: rest, a few units of z's last place, comes back in the same factor.
+    __device__ Logistic(float z, float rest)
+    {
+        const float w = fminf(fabsf(z), 256.0f), u = __fmul_rn(w, -kHalfLog2e);
         const float lo = __fmaf_rn(w, -kHalfLog2eRest, __fmaf_rn(w, -kHalfLog2e, -u));
+        take(z, u, __fmaf_rn(z < 0.0f ? rest : -rest, kHalfLog2e, lo));
+    }
+    __device__ __forceinline__ void take(float z, float u, float lo)
+    {
         float p;
         asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(p) : "f"(u));
         h = __fmaf_rn(p, __fmul_rn(lo, 0.69314718055994531f), p);
@@ -52,6 +62,21 @@ struct Logistic {
 
 template <int ACT>
 __device__ __forceinline__ float act_argument(float x) { return ACT == SPARQ_ACT_SILU ? x : kGeluScale * x * __fmaf_rn(kGeluCubic * x, x, 1.0f); }
+
+// GELU to a few units of the last place.  An error of the argument is a relative one of the result, and what the argument's roundings in fp32 make of it is 72 units of 2^-23 near x = -9 (37 near -7, 16 near -5).  So
+// the argument comes in two parts, its rounded value and what the roundings, the constants' among them, left of it.
+constexpr float kGeluScaleRest = -4.5340680e-8f, kGeluCubicRest = 1.5461445e-9f;
+__device__ __forceinline__ float gelu_exact(float x)
+{
+    const float c = fminf(fmaxf(x, -64.0f), 64.0f);        // s is 0 or 1 to the last bit long before
+    const float t = __fmul_rn(c, c), t_rest = __fmaf_rn(c, c, -t);
+    const float a = __fmul_rn(kGeluCubic, t), a_rest = __fadd_rn(__fmaf_rn(kGeluCubic, t, -a), __fmaf_rn(kGeluCubic, t_rest, __fmul_rn(kGeluCubicRest, t)));
+    const float q = __fadd_rn(1.0f, a), back = __fsub_rn(q, 1.0f);
+    const float q_rest = __fadd_rn(__fadd_rn(__fsub_rn(1.0f, __fsub_rn(q, back)), __fsub_rn(a, back)), a_rest);
+    const float u = __fmul_rn(kGeluScale, c), u_rest = __fmaf_rn(kGeluScaleRest, c, __fmaf_rn(kGeluScale, c, -u));
+    const float z = __fmul_rn(u, q), z_rest = __fadd_rn(__fmaf_rn(u, q, -z), __fmaf_rn(u, q_rest, __fmul_rn(u_rest, q)));
+    return Logistic(z, z_rest).times(x);
+}
 
 template <bool BF16, int ACT>
 __device__ __forceinline__ float act_value(float x)

@@ -219,7 +219,7 @@ __device__ __forceinline__ void lin_act(float (&y)[C], int act)
             lin_logistic<SPARQ_ACT_GELU>(y);
         } else {
 #pragma unroll
-            for (int j = 0; j < C; ++j) y[j] = act_value<FAST, SPARQ_ACT_GELU>(y[j]);
+            for (int j = 0; j < C; ++j) y[j] = FAST ? act_value<FAST, SPARQ_ACT_GELU>(y[j]) : gelu_exact(y[j]);
         }
     }
 }
