@@ -238,7 +238,6 @@ extern "C" int sparq_linear(const void *x, int64_t ldx, const void *w, int64_t l
     g.ldr = ldr;
     g.out = e->out;
     g.ldo = ldo;
-    g.out_dt = e->out_dtype;
     g.z_codes = e->z_codes;
     g.z_scales = e->z_scales;
     g.z_pitch = mx_code_pitch(SPARQ_MXINT8, N);

@@ -29,7 +29,6 @@ struct LinArgs {
     int64_t ldr;
     void *out;
     int64_t ldo;
-    int out_dt;
     int8_t *z_codes;
     uint8_t *z_scales;
     int64_t z_pitch, z_spitch;

@@ -173,10 +173,13 @@ __device__ __forceinline__ void store_elements(uint8_t *b, const uint32_t (&v)[k
 // where there is nothing to store.  ALIGN 0: each lane stores the aligned vectors that begin in front of its run and so takes the end
 // of its left neighbour's; what has no neighbour to take it goes element by element.
 template <bool BF16, int ALIGN>
-__device__ __forceinline__ void store_words(void *p, const uint32_t (&v)[kRunWords<BF16>], int64_t left, int64_t run)
+__device__ __forceinline__ void store_run(void *p, const float (&f)[16], int64_t left, int64_t run)
 {
     constexpr int W = kRunWords<BF16>;
     uint8_t *b = reinterpret_cast<uint8_t *>(p);
+    uint32_t v[W];
+#pragma unroll
+    for (int i = 0; i < W; ++i) v[i] = BF16 ? bf16x2_of(f[2 * i % 16], f[(2 * i + 1) % 16]) : __float_as_uint(f[i]);
     if (ALIGN >= 16) {
         if (left >= 16) {
 #pragma unroll
@@ -213,15 +216,6 @@ __device__ __forceinline__ void store_words(void *p, const uint32_t (&v)[kRunWor
 #pragma unroll
     for (int i = 4; i < W; i += 4) st_v4(b - s + 4 * i, w + i);
     if (!taken) store_elements<BF16>(b, v, 16 - (int)s / per, 16);
-}
-
-template <bool BF16, int ALIGN>
-__device__ __forceinline__ void store_run(void *p, const float (&f)[16], int64_t left, int64_t run)
-{
-    uint32_t v[kRunWords<BF16>];
-#pragma unroll
-    for (int i = 0; i < kRunWords<BF16>; ++i) v[i] = BF16 ? bf16x2_of(f[2 * i % 16], f[(2 * i + 1) % 16]) : __float_as_uint(f[i]);
-    store_words<BF16, ALIGN>(p, v, left, run);
 }
 
 // ---- blocks ------------------------------------------------------------------------------------
