@@ -87,3 +87,38 @@ def test_around_the_ends_of_pieces(m, n, k):
     y = (x.to(F64) @ w.to(F64).T + bias.to(F64)).clamp(min=0.0) + res.to(F64)
     inside(out, y, sum_error(size_of, k, torch.float32) + 2.0 ** -24 * y.abs() + 1e-30)
 
+
+
+@pytest.mark.parametrize("m,n,k", [(20, 264, 9000), (150, 1000, 1500), (900, 2056, 1500)])
+def test_same_bits_captured_and_on_two_streams(m, n, k):
+    dt = torch.bfloat16
+    x, w, bias, res = matrix(m, k, dt, 1), matrix(n, k, dt, 2, k ** -0.5), torch.randn(n, device="cuda"), matrix(m, n, torch.float32, 3, pitch=n)
+
+    def step():
+        out, half = room(m, n, torch.float32), room(m, n, dt)
+        codes = torch.empty((m, -(-n // 32) * 32), dtype=torch.int8, device="cuda")
+        scales = torch.empty((sparq.sparq_mx_scale_bytes(sparq.FORMAT_MXINT8, m, n),), dtype=torch.uint8, device="cuda")
+        sparq.sparq_linear(x, w, out, bias=bias, act=3, residual=res)
+        sparq.sparq_linear(x, w, half, bias=bias, act=2, z_codes=codes, z_scales=scales)
+        return out, half, codes, scales
+
+    first = step()
+    streams, others = [torch.cuda.Stream(), torch.cuda.Stream()], []
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(4):
+        for s in streams:
+            with torch.cuda.stream(s):
+                others.append(step())
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        recorded = step()
+    for t in recorded:
+        t.zero_()
+    graph.replay()
+    graph.replay()
+    torch.cuda.synchronize()
+    for other in others + [recorded]:
+        assert all(torch.equal(a, b) for a, b in zip(first, other))
+    sparq.sparq_check()
