@@ -442,6 +442,7 @@ typedef struct {
  * time and cut the running sum off where rounding would be to nearest; sums therefore run over pieces of P elements of K, which are added rounded to nearest: terms of one sign lose up to P / 16 units
  * of 2^-23.  With fp32 outputs or z kept P is 12 sqrt(K), 1024 at the most (fp32 outputs are off by 3e-7 at K = 1024 and 6e-7 at 4096, 2-norm, an fp32 product by 2e-7 and 5e-7); else it is
  * 8192, which 16 bits do not show (2^-14).  A row's outputs are, to the last bit, a matter of that row and the weights: not of the rows beside it or of what lies where an expert has none.
+ * Matrices of experts do not reach into one another: w_stride is at least (rows of w - 1) * ldw + its columns.
  * Requirements (else SPARQ_ERR_UNSUPPORTED): x and w 16-byte aligned, ldx, ldw and w_stride multiples of 8 (ldx of a single row is not
  * looked at), out, residual and bias aligned to their elements, z_codes and z_scales to 16 bytes, M, N and K below 2^31 - 256. */
 SPARQ_API int sparq_linear(const void *x, int64_t ldx, const void *w, int64_t ldw, int64_t w_stride, int transposed, int dtype,
@@ -467,7 +468,8 @@ SPARQ_API int sparq_linear_wgrad(const void *dy, int64_t lddy, const void *x, in
 SPARQ_API int sparq_expert_sort(const int32_t *experts, int64_t T, int64_t k, int64_t E, int32_t *offsets, int32_t *position, void *stream);
 
 /* xs[position[t][j]] = x[t] for every choice that is not dropped: x is T x cols, xs has T * k rows, of which those that
- * no position names are left as they are.  dtype: any SPARQ_DTYPE_*.  Positions outside 0 .. T * k - 1 are dropped choices.
+ * no position names are left as they are.  dtype: any SPARQ_DTYPE_*.  Positions outside 0 .. T * k - 1 are dropped choices; a row that
+ * two of them name is undefined (here and in dys below).
  * Its gradient is sparq_expert_combine without weights.  In these three calls pointers are aligned to their elements (32-byte aligned
  * rows are fastest), inputs and outputs do not overlap, and T == 0, k == 0 or cols == 0 is a no-op but for what is said below. */
 SPARQ_API int sparq_expert_gather(const void *x, int dtype, int64_t T, int64_t k, int64_t cols, int64_t ldx, const int32_t *position,
